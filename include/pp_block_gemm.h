@@ -56,6 +56,11 @@ typedef struct {
  * unknown dtype, flag or variant, or variant 2 with PP_F32. */
 pp_status_t pp_block_gemm_plan(const pp_block_gemm_desc_t *desc, pp_block_gemm_plan_t **out_plan);
 
+/* A plan of the transposed weights: desc describes Wd (m x k), the plan multiplies by Wd^T (its m is desc's k and its k is
+ * desc's m), which is how a gradient with respect to y becomes one with respect to x.  desc's bias is not read and PP_FLAG_RELU
+ * does not apply.  Otherwise as pp_block_gemm_plan. */
+pp_status_t pp_block_gemm_plan_transposed(const pp_block_gemm_desc_t *desc, pp_block_gemm_plan_t **out_plan);
+
 /* Enqueue y = act(Wd x + bias) for n columns.
  *   x_dev : [k][n] row-major, plan dtype, 16-byte aligned, caller-owned
  *   y_dev : [m][n] row-major, plan dtype, 16-byte aligned, caller-owned, must not overlap x_dev

@@ -44,23 +44,25 @@ void release(pp_block_gemm_plan_t* p) {
 struct K4Shape {
     int cols;                                                  // columns of a workgroup
     void (*launch)(const K4Args& a, int blocks, hipStream_t stream);
+    void (*launch_adapted)(const K4AdaptedArgs& a, int blocks, hipStream_t stream);
 };
 
-template <bool RAGGED> void launch_wide_as(const K4Args& a, int blocks, hipStream_t stream) {
-    static const hipError_t lds_attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k4_block_gemm<RAGGED>), hipFuncAttributeMaxDynamicSharedMemorySize, kK4LdsBytes);
+template <bool RAGGED, typename Args> void launch_wide_as(const Args& a, int blocks, hipStream_t stream) {
+    static const hipError_t lds_attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k4_block_gemm<RAGGED, Args>), hipFuncAttributeMaxDynamicSharedMemorySize, kK4LdsBytes);
     (void)lds_attr;
-    hipLaunchKernelGGL(k4_block_gemm<RAGGED>, dim3((unsigned)blocks), dim3(256), kK4LdsBytes, stream, a);
+    hipLaunchKernelGGL((k4_block_gemm<RAGGED, Args>), dim3((unsigned)blocks), dim3(256), kK4LdsBytes, stream, a);
 }
-void launch_wide(const K4Args& a, int blocks, hipStream_t stream) {
+template <typename Args> void launch_wide(const Args& a, int blocks, hipStream_t stream) {
     if (a.ragged) launch_wide_as<true>(a, blocks, stream);
     else launch_wide_as<false>(a, blocks, stream);
 }
-template <int NT, int WK> void launch_split(const K4Args& a, int blocks, hipStream_t stream) {
+template <int NT, int WK, typename Args> void launch_split(const Args& a, int blocks, hipStream_t stream) {
     constexpr int lds = k4_split_lds_bytes(NT, WK);
-    static const hipError_t lds_attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k4_split<NT, WK>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    static const hipError_t lds_attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&k4_split<NT, WK, Args>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     (void)lds_attr;
-    hipLaunchKernelGGL((k4_split<NT, WK>), dim3((unsigned)blocks), dim3(64 * WK), lds, stream, a);
+    hipLaunchKernelGGL((k4_split<NT, WK, Args>), dim3((unsigned)blocks), dim3(64 * WK), lds, stream, a);
 }
+template <int NT, int WK> K4Shape split_shape() { return {32 * NT, launch_split<NT, WK, K4Args>, launch_split<NT, WK, K4AdaptedArgs>}; }
 
 // Which tile a launch runs with: the smallest modelled time.  A workgroup of the split kernel walks chunks / wk chunks per
 // wavefront, each worth 0.14 us of latency and, for every wavefront on the compute unit, nt + 2 KB through the vector cache
@@ -71,9 +73,9 @@ template <int NT, int WK> void launch_split(const K4Args& a, int blocks, hipStre
 // 181 columns: 1 x 8 4.6 us, 512-column tile 9.8.
 K4Shape k4_pick(const BlockHostPlan& hp, int n, int batch) {
     struct Split { int nt, wk, resident; K4Shape shape; };
-    static const Split kSplits[] = {{1, 4, 4, {32, launch_split<1, 4>}}, {1, 8, 2, {32, launch_split<1, 8>}}, {2, 4, 3, {64, launch_split<2, 4>}},
-                                    {2, 8, 1, {64, launch_split<2, 8>}}, {4, 4, 2, {128, launch_split<4, 4>}}, {4, 8, 1, {128, launch_split<4, 8>}}};
-    const K4Shape wide{kBlockColTile, launch_wide};
+    static const Split kSplits[] = {{1, 4, 4, split_shape<1, 4>()}, {1, 8, 2, split_shape<1, 8>()}, {2, 4, 3, split_shape<2, 4>()},
+                                    {2, 8, 1, split_shape<2, 8>()}, {4, 4, 2, split_shape<4, 4>()}, {4, 8, 1, split_shape<4, 8>()}};
+    const K4Shape wide{kBlockColTile, launch_wide<K4Args>, launch_wide<K4AdaptedArgs>};
     if (hp.k >= (1 << 24) || n >= (1 << 23)) return wide;       // the split kernel multiplies in 24 bits
     const double chunks = (double)hp.tile_cols.size() / kBlockChunk / hp.row_tiles;
     auto wgs = [&](int cols) { return (int64_t)hp.row_tiles * ((n + cols - 1) / cols) * batch; };
@@ -92,13 +94,13 @@ K4Shape k4_pick(const BlockHostPlan& hp, int n, int batch) {
 
 }  // namespace
 
-pp_status_t pp_block_gemm_launch_batched(const pp_block_gemm_plan_t* plan, const void* x_dev, void* y_dev, int32_t n, int32_t batch, int64_t x_stride,
-                                         int64_t y_stride, void* hip_stream) {
+static pp_status_t launch_f16(const pp_block_gemm_plan_t* plan, const void* x_dev, void* y_dev, int32_t n, int32_t batch, int64_t x_stride, int64_t y_stride,
+                              const K4Expand* expand, void* hip_stream) {
     if (!plan || !x_dev || !y_dev) return PP_ERR_NULL;
     const BlockHostPlan& hp = plan->hp;
     if (n < 1 || batch < 1 || hp.dtype != PP_F16 || !plan->on_device) return PP_ERR_UNSUPPORTED;
     if ((int64_t)hp.k * n >= ((int64_t)1 << 31) || (int64_t)hp.m * n >= ((int64_t)1 << 31)) return PP_ERR_SHAPE;
-    K4Args a;
+    K4AdaptedArgs a;
     a.x = x_dev, a.y = y_dev, a.apk = plan->d_apk, a.bias = plan->d_bias;
     a.tile_off = plan->d_tile_off, a.tile_cols = plan->d_tile_cols;
     a.m = hp.m, a.n = n, a.row_tiles = hp.row_tiles;
@@ -113,19 +115,29 @@ pp_status_t pp_block_gemm_launch_batched(const pp_block_gemm_plan_t* plan, const
     a.items = (int)items;
     a.per_xcd = (a.items + 7) / 8;
     (void)hipGetLastError();
-    sh.launch(a, a.per_xcd * 8, static_cast<hipStream_t>(hip_stream));
+    if (expand) {
+        a.expand = *expand;
+        sh.launch_adapted(a, a.per_xcd * 8, static_cast<hipStream_t>(hip_stream));
+    } else {
+        sh.launch(a, a.per_xcd * 8, static_cast<hipStream_t>(hip_stream));
+    }
     return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_DEVICE;
 }
 
+pp_status_t pp_block_gemm_launch_batched(const pp_block_gemm_plan_t* plan, const void* x_dev, void* y_dev, int32_t n, int32_t batch, int64_t x_stride,
+                                         int64_t y_stride, void* hip_stream) {
+    return launch_f16(plan, x_dev, y_dev, n, batch, x_stride, y_stride, nullptr, hip_stream);
+}
+
 // Binary32 on the matrix cores.  PP_ERR_UNSUPPORTED if x does not fit 31-bit byte offsets.
-static pp_status_t launch_list_f32(const pp_block_gemm_plan_t* plan, const void* x_dev, void* y_dev, int32_t n, hipStream_t stream) {
+static pp_status_t launch_list_f32(const pp_block_gemm_plan_t* plan, const void* x_dev, void* y_dev, int32_t n, int relu, hipStream_t stream) {
     const BlockHostPlan& hp = plan->hp;
     K5ListArgs a{};
     a.x_bytes = (int64_t)hp.k * n * 4;
     if (a.x_bytes >= ((int64_t)1 << 31)) return PP_ERR_UNSUPPORTED;
     a.x = static_cast<const float*>(x_dev), a.y = static_cast<float*>(y_dev);
     a.wpk = plan->d_wpk32, a.bias = plan->d_bias, a.list = plan->d_list32, a.group_off = plan->d_group_off32;
-    a.m = hp.m, a.n = n, a.relu = (hp.flags & PP_FLAG_RELU) ? 1 : 0;
+    a.m = hp.m, a.n = n, a.relu = relu;
     a.row_tiles = (hp.m + kBlockRow32 - 1) / kBlockRow32;
     const K5Shape sh = k5_pick_list(a.row_tiles, n, hp.group_off32.back() / a.row_tiles);
     a.col_tiles = (n + 32 * sh.nt - 1) / (32 * sh.nt);
@@ -139,15 +151,58 @@ static pp_status_t launch_list_f32(const pp_block_gemm_plan_t* plan, const void*
     return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_DEVICE;
 }
 
-extern "C" {
+// Plans of variant 1, any n.
+static pp_status_t launch_lists(const pp_block_gemm_plan_t* plan, const void* x_dev, void* y_dev, int32_t n, int relu, hipStream_t stream) {
+    const BlockHostPlan& hp = plan->hp;
+    (void)hipGetLastError();
+    if (hp.dtype == PP_F32) {
+        const pp_status_t st = launch_list_f32(plan, x_dev, y_dev, n, relu, stream);
+        if (st != PP_ERR_UNSUPPORTED) return st;
+    }
+    {
+        const dim3 grid((unsigned)((n + 63) / 64), (unsigned)hp.row_tiles), block(64, 4);
+        if (hp.row_tiles > 65535) return PP_ERR_SHAPE;
+        if (hp.dtype == PP_F16)
+            hipLaunchKernelGGL(k4_generic<_Float16>, grid, block, 0, stream, static_cast<const _Float16*>(x_dev), static_cast<_Float16*>(y_dev),
+                               plan->d_wpk32, plan->d_bias, plan->d_group_off32, plan->d_list32, hp.m, n, relu);
+        else
+            hipLaunchKernelGGL(k4_generic<float>, grid, block, 0, stream, static_cast<const float*>(x_dev), static_cast<float*>(y_dev), plan->d_wpk32,
+                               plan->d_bias, plan->d_group_off32, plan->d_list32, hp.m, n, relu);
+    }
+    return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_DEVICE;
+}
 
-pp_status_t pp_block_gemm_plan(const pp_block_gemm_desc_t* desc, pp_block_gemm_plan_t** out_plan) {
+namespace ppc {
+
+BlockPlanFacts block_plan_facts(const pp_block_gemm_plan_t* plan) {
+    return {plan->hp.m, plan->hp.k, plan->hp.dtype, (plan->hp.flags & PP_FLAG_RELU) ? 1 : 0};
+}
+
+pp_status_t block_check_adapted(const pp_block_gemm_plan_t* plan, int32_t n) {
+    const BlockHostPlan& hp = plan->hp;
+    if (hp.dtype == PP_F16 && hp.variant != 2) return PP_ERR_UNSUPPORTED;
+    if (hp.variant == 2 && hp.forced && (n % 8) != 0) return PP_ERR_UNSUPPORTED;
+    if (hp.dtype == PP_F32 && hp.row_tiles > 65535 && (int64_t)hp.k * n * 4 >= ((int64_t)1 << 31)) return PP_ERR_SHAPE;
+    return plan->on_device ? PP_OK : PP_ERR_UNSUPPORTED;
+}
+
+pp_status_t block_launch_adapted(const pp_block_gemm_plan_t* plan, const void* x_dev, void* y_dev, int32_t n, const K4Expand& expand, void* hip_stream) {
+    return launch_f16(plan, x_dev, y_dev, n, 1, 0, 0, &expand, hip_stream);
+}
+
+pp_status_t block_launch_linear_f32(const pp_block_gemm_plan_t* plan, const void* x_dev, void* y_dev, int32_t n, void* hip_stream) {
+    return launch_lists(plan, x_dev, y_dev, n, 0, static_cast<hipStream_t>(hip_stream));
+}
+
+}  // namespace ppc
+
+static pp_status_t make_plan(const pp_block_gemm_desc_t* desc, bool transposed, pp_block_gemm_plan_t** out_plan) {
     if (out_plan) *out_plan = nullptr;
     if (!desc || !out_plan) return PP_ERR_NULL;
     pp_block_gemm_plan_t* p = nullptr;
     try {
         p = new pp_block_gemm_plan_t();
-        const pp_status_t st = build_block_plan(*desc, p->hp);
+        const pp_status_t st = transposed ? build_block_plan_transposed(*desc, p->hp) : build_block_plan(*desc, p->hp);
         if (st != PP_OK) {
             delete p;
             return st;
@@ -179,6 +234,12 @@ pp_status_t pp_block_gemm_plan(const pp_block_gemm_desc_t* desc, pp_block_gemm_p
     return PP_OK;
 }
 
+extern "C" {
+
+pp_status_t pp_block_gemm_plan(const pp_block_gemm_desc_t* desc, pp_block_gemm_plan_t** out_plan) { return make_plan(desc, false, out_plan); }
+
+pp_status_t pp_block_gemm_plan_transposed(const pp_block_gemm_desc_t* desc, pp_block_gemm_plan_t** out_plan) { return make_plan(desc, true, out_plan); }
+
 pp_status_t pp_block_gemm_run(const pp_block_gemm_plan_t* plan, const void* x_dev, void* y_dev, int32_t n, void* hip_stream) {
     if (!plan || !x_dev || !y_dev) return PP_ERR_NULL;
     const BlockHostPlan& hp = plan->hp;
@@ -190,25 +251,8 @@ pp_status_t pp_block_gemm_run(const pp_block_gemm_plan_t* plan, const void* x_de
     if (xa < ye && ya < xe) return PP_ERR_ALIGN;
     if (hp.variant == 2 && hp.forced && (n % 8) != 0) return PP_ERR_UNSUPPORTED;        // what the header promises of a forced variant
     if (!plan->on_device) return PP_ERR_UNSUPPORTED;
-    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const int relu = (hp.flags & PP_FLAG_RELU) ? 1 : 0;
-    (void)hipGetLastError();
     if (hp.variant == 2) return pp_block_gemm_launch_batched(plan, x_dev, y_dev, n, 1, 0, 0, hip_stream);
-    if (hp.dtype == PP_F32) {
-        const pp_status_t st = launch_list_f32(plan, x_dev, y_dev, n, stream);
-        if (st != PP_ERR_UNSUPPORTED) return st;
-    }
-    {
-        const dim3 grid((unsigned)((n + 63) / 64), (unsigned)hp.row_tiles), block(64, 4);
-        if (hp.row_tiles > 65535) return PP_ERR_SHAPE;
-        if (hp.dtype == PP_F16)
-            hipLaunchKernelGGL(k4_generic<_Float16>, grid, block, 0, stream, static_cast<const _Float16*>(x_dev), static_cast<_Float16*>(y_dev),
-                               plan->d_wpk32, plan->d_bias, plan->d_group_off32, plan->d_list32, hp.m, n, relu);
-        else
-            hipLaunchKernelGGL(k4_generic<float>, grid, block, 0, stream, static_cast<const float*>(x_dev), static_cast<float*>(y_dev), plan->d_wpk32,
-                               plan->d_bias, plan->d_group_off32, plan->d_list32, hp.m, n, relu);
-    }
-    return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_DEVICE;
+    return launch_lists(plan, x_dev, y_dev, n, (hp.flags & PP_FLAG_RELU) ? 1 : 0, static_cast<hipStream_t>(hip_stream));
 }
 
 pp_status_t pp_block_gemm_destroy(pp_block_gemm_plan_t* plan) {

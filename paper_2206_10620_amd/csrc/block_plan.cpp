@@ -126,6 +126,37 @@ pp_status_t build_block_plan(const pp_block_gemm_desc_t& d, BlockHostPlan& p) {
     return PP_OK;
 }
 
+pp_status_t build_block_plan_transposed(const pp_block_gemm_desc_t& d, BlockHostPlan& p) {
+    if (!d.weights) return PP_ERR_NULL;
+    if (d.m < 1 || d.k < 1 || d.block_m < 1 || d.block_k < 1) return PP_ERR_SHAPE;
+    if ((int64_t)d.m * d.k >= ((int64_t)1 << 31)) return PP_ERR_SHAPE;
+    if (d.flags & ~(uint32_t)(PP_FLAG_RELU | PP_FLAG_HOST_ONLY)) return PP_ERR_UNSUPPORTED;
+    std::vector<float> w((size_t)d.m * d.k);
+    constexpr int T = 32;                                // tile by tile: both sides stay in cache
+    for (int r0 = 0; r0 < d.m; r0 += T)
+        for (int c0 = 0; c0 < d.k; c0 += T)
+            for (int c = c0; c < std::min(d.k, c0 + T); ++c)
+                for (int r = r0; r < std::min(d.m, r0 + T); ++r) w[(size_t)c * d.m + r] = d.weights[(size_t)r * d.k + c];
+    // block (bi, bj) becomes (bj, bi), and what was a row of it a column
+    const int64_t bm = ((int64_t)d.m + d.block_m - 1) / d.block_m, bk = ((int64_t)d.k + d.block_k - 1) / d.block_k;
+    std::vector<uint8_t> rows, cols;
+    auto swap = [&](const uint8_t* from, int64_t width, std::vector<uint8_t>& to) {
+        if (!from) return;
+        to.resize((size_t)(bm * bk * width));
+        for (int64_t bi = 0; bi < bm; ++bi)
+            for (int64_t bj = 0; bj < bk; ++bj) std::memcpy(&to[(size_t)((bj * bm + bi) * width)], from + (bi * bk + bj) * width, (size_t)width);
+    };
+    swap(d.col_keep, d.block_k, rows);
+    swap(d.row_keep, d.block_m, cols);
+    pp_block_gemm_desc_t t = d;
+    t.m = d.k, t.k = d.m, t.block_m = d.block_k, t.block_k = d.block_m;
+    t.row_keep = rows.empty() ? nullptr : rows.data();
+    t.col_keep = cols.empty() ? nullptr : cols.data();
+    t.weights = w.data(), t.bias = nullptr;
+    t.flags = d.flags & ~(uint32_t)PP_FLAG_RELU;
+    return build_block_plan(t, p);
+}
+
 pp_status_t unpack_block_tile(const BlockHostPlan& p, int tile, float* w_out) {
     if (tile < 0 || tile >= p.row_tiles) return PP_ERR_SHAPE;
     const int RT = kBlockRowTile;

@@ -38,6 +38,8 @@ struct BlockHostPlan {
 
 // Validates the description and builds the plan.  No device call.
 pp_status_t build_block_plan(const pp_block_gemm_desc_t& d, BlockHostPlan& out);
+// The same for the transposed matrix; `d` describes the untransposed one.
+pp_status_t build_block_plan_transposed(const pp_block_gemm_desc_t& d, BlockHostPlan& out);
 // Decodes row tile `tile` back to a dense [64][k] matrix from the packed form the plan's kernel reads.
 pp_status_t unpack_block_tile(const BlockHostPlan& p, int tile, float* w_out);
 
@@ -48,3 +50,17 @@ pp_status_t unpack_block_tile(const BlockHostPlan& p, int tile, float* w_out);
 // likewise y ([m][n]).  Binary16 matrix-core kernels only, any n; used by the convolution library for 1x1 layers.
 pp_status_t pp_block_gemm_launch_batched(const pp_block_gemm_plan_t* plan, const void* x_dev, void* y_dev, int32_t n, int32_t batch, int64_t x_stride,
                                          int64_t y_stride, void* hip_stream);
+
+namespace ppc {
+struct K4Expand;
+
+// What the adapters need of a product: its sizes (PP_ERR_UNSUPPORTED for a host-only plan or a forced variant that does not take n),
+// and its launch, with the adapters' part added before act (binary16), or without act, which whoever adds them applies (binary32).
+struct BlockPlanFacts {
+    int m, k, dtype, relu;
+};
+BlockPlanFacts block_plan_facts(const pp_block_gemm_plan_t* plan);
+pp_status_t block_check_adapted(const pp_block_gemm_plan_t* plan, int32_t n);
+pp_status_t block_launch_adapted(const pp_block_gemm_plan_t* plan, const void* x_dev, void* y_dev, int32_t n, const K4Expand& expand, void* hip_stream);
+pp_status_t block_launch_linear_f32(const pp_block_gemm_plan_t* plan, const void* x_dev, void* y_dev, int32_t n, void* hip_stream);
+}  // namespace ppc

@@ -20,6 +20,7 @@
 
 #include "block_plan.hpp"
 #include "block_rules.hpp"
+#include "k4_expand.hpp"
 
 namespace ppc {
 
@@ -35,6 +36,11 @@ struct K4Args {
     uint32_t x_bytes;           // k * n * 2: one matrix of x
     // a batch of products with the same weights (the images of a 1x1 convolution): item = (image, column tile, row tile)
     int64_t x_stride, y_stride;  // elements between the x (y) matrices of consecutive images
+};
+
+// the same product with the adapters' part added (batch 1): a type of its own, and so a kernel of its own
+struct K4AdaptedArgs : K4Args {
+    K4Expand expand;
 };
 
 constexpr int kK4Stages = 4;
@@ -95,8 +101,8 @@ __device__ __forceinline__ void k4_wait_vm(int n) {
 }
 
 // RAGGED: n is not a multiple of 8 (a variant of its own: the checks cost the aligned case 5 %, 66.5 -> 70 us on 4096 columns)
-template <bool RAGGED>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k4_block_gemm(const K4Args a) {
+template <bool RAGGED, typename Args = K4Args>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k4_block_gemm(const Args a) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char k4_smem[];
     constexpr int NS = kK4Stages, NT = 4;
     const int lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
@@ -222,6 +228,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
         for (int c = 0; c < NS; ++c)
             if (c < nch) issue(c, c);
+    }
+    // while the first chunks are on their way
+    if constexpr (std::is_same<Args, K4AdaptedArgs>::value) k4_expand<NT>(a.expand, acc, col0 + wave * 128, a.n, rt, lane, 0, 1);
+    if (nch > 0) {
         k4_wait_vm(RAGGED && drain ? 0 : (nch > NS ? NS - 1 : nch - 1) * (wload ? 5 : 4));
         __syncthreads();
         read_frags(0, 0);
@@ -295,8 +305,8 @@ constexpr int k4_split_lds_bytes(int nt, int wk) {
     return ring > sum ? ring : sum;
 }
 
-template <int NT, int WK>
-__global__ __launch_bounds__(64 * WK) __attribute__((amdgpu_waves_per_eu(2))) void k4_split(const K4Args a) {
+template <int NT, int WK, typename Args = K4Args>
+__global__ __launch_bounds__(64 * WK) __attribute__((amdgpu_waves_per_eu(2))) void k4_split(const Args a) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char k4_smem[];
     constexpr int NS = kK4SplitStages, PPR = 4 * NT, RPI = 16 / NT, SB = k4_split_stage_bytes(NT), CI = NT + 2;
     const int lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
@@ -402,6 +412,10 @@ __global__ __launch_bounds__(64 * WK) __attribute__((amdgpu_waves_per_eu(2))) vo
         for (int c = 0; c < NS; ++c)
             if (c < nch) issue(c, c);
         if (nch > 8) issue_list(1);                          // segment s + 1 is fetched eight chunks ahead of its first use
+    }
+    // while the first chunks are on their way; the wavefronts deal the slots out among them, their sums are added anyway
+    if constexpr (std::is_same<Args, K4AdaptedArgs>::value) k4_expand<NT>(a.expand, acc, col0, a.n, rt, lane, wave, WK);
+    if (nch > 0) {
         k4_wait_vm(drain ? 0 : (nch > NS ? NS - 1 : nch - 1) * CI);
         read_frags(0, 0);
         int stage = 0;

@@ -37,6 +37,8 @@ def lib() -> C.CDLL:
         vp = C.c_void_p
         L.pp_block_gemm_plan.argtypes = [C.POINTER(_Desc), C.POINTER(vp)]
         L.pp_block_gemm_plan.restype = C.c_int
+        L.pp_block_gemm_plan_transposed.argtypes = [C.POINTER(_Desc), C.POINTER(vp)]
+        L.pp_block_gemm_plan_transposed.restype = C.c_int
         L.pp_block_gemm_run.argtypes = [vp, vp, vp, C.c_int32, vp]
         L.pp_block_gemm_run.restype = C.c_int
         L.pp_block_gemm_destroy.argtypes = [vp]
@@ -53,16 +55,25 @@ def _ptr(a: Optional[np.ndarray]):
     return None if a is None else a.ctypes.data_as(C.c_void_p)
 
 
-def pp_block_gemm_plan(m, k, block_m, block_k, row_keep, col_keep, weights, bias=None, flags=0, dtype=PP_F16, variant=0):
-    """Returns (status, handle)."""
+def _plan(entry, m, k, block_m, block_k, row_keep, col_keep, weights, bias, flags, dtype, variant):
     rk = None if row_keep is None else np.ascontiguousarray(row_keep, dtype=np.uint8)
     ck = None if col_keep is None else np.ascontiguousarray(col_keep, dtype=np.uint8)
     w = None if weights is None else np.ascontiguousarray(weights, dtype=np.float32)
     b = None if bias is None else np.ascontiguousarray(bias, dtype=np.float32)
     d = _Desc(m, k, block_m, block_k, _ptr(rk), _ptr(ck), _ptr(w), _ptr(b), flags, dtype, variant)
     h = C.c_void_p()
-    st = lib().pp_block_gemm_plan(C.byref(d), C.byref(h))
+    st = entry(C.byref(d), C.byref(h))
     return st, (h if st == PP_OK else None)
+
+
+def pp_block_gemm_plan(m, k, block_m, block_k, row_keep, col_keep, weights, bias=None, flags=0, dtype=PP_F16, variant=0):
+    """Returns (status, handle)."""
+    return _plan(lib().pp_block_gemm_plan, m, k, block_m, block_k, row_keep, col_keep, weights, bias, flags, dtype, variant)
+
+
+def pp_block_gemm_plan_transposed(m, k, block_m, block_k, row_keep, col_keep, weights, bias=None, flags=0, dtype=PP_F16, variant=0):
+    """Returns (status, handle): a plan that multiplies by the transpose of the weights described."""
+    return _plan(lib().pp_block_gemm_plan_transposed, m, k, block_m, block_k, row_keep, col_keep, weights, bias, flags, dtype, variant)
 
 
 def pp_block_gemm_run(plan, x_dev: int, y_dev: int, n: int, hip_stream: int = 0) -> int:
@@ -134,12 +145,22 @@ class BlockPlan:
             pass
 
 
-def block_plan_from_layer(layer, host_only=False, variant=0) -> BlockPlan:
-    """Plan for a block-layer description object (fields as in synth.BlockLayer)."""
+def _from_layer(entry, name, layer, host_only, variant):
     flags = (PP_FLAG_RELU if layer.relu else 0) | (PP_FLAG_HOST_ONLY if host_only else 0)
     dtype = PP_F16 if layer.dtype == "f16" else PP_F32
-    st, h = pp_block_gemm_plan(layer.m, layer.k, layer.bm, layer.bk, layer.row_keep, layer.col_keep, layer.weights, layer.bias,
-                               flags, dtype, variant)
+    st, h = entry(layer.m, layer.k, layer.bm, layer.bk, layer.row_keep, layer.col_keep, layer.weights, layer.bias, flags, dtype, variant)
     if st != PP_OK:
-        raise PPError(st, "pp_block_gemm_plan")
+        raise PPError(st, name)
+    return h, dtype
+
+
+def block_plan_from_layer(layer, host_only=False, variant=0) -> BlockPlan:
+    """Plan for a block-layer description object (fields as in synth.BlockLayer)."""
+    h, dtype = _from_layer(pp_block_gemm_plan, "pp_block_gemm_plan", layer, host_only, variant)
     return BlockPlan(h, layer.m, layer.k, dtype)
+
+
+def block_plan_transposed_from_layer(layer, host_only=False, variant=0) -> BlockPlan:
+    """Plan for the transposed weights of such an object: gradients with respect to its output become those with respect to its input."""
+    h, dtype = _from_layer(pp_block_gemm_plan_transposed, "pp_block_gemm_plan_transposed", layer, host_only, variant)
+    return BlockPlan(h, layer.k, layer.m, dtype)

@@ -23,8 +23,7 @@ template <typename T> __global__ __launch_bounds__(256) void act8_pack(const Act
     for (int64_t unit = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4); unit < a.units; unit += (int64_t)gridDim.x * 16) {
         const int row = (int)(unit / a.blocks), b = (int)(unit - (int64_t)row * a.blocks);
         const int t = b * kAct8Block + part * 8;
-        T v[8];
-        k8_load<T, 8>(static_cast<const T*>(a.x) + (int64_t)row * a.n + t, a.n - t, v);
+        const k8_any<T, 8> v = k8_load<T, 8>(static_cast<const T*>(a.x) + (int64_t)row * a.n + t, a.n - t);
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -62,7 +61,7 @@ template <typename T> __global__ __launch_bounds__(256) void act8_unpack(const A
         const uint2 q = *reinterpret_cast<const uint2*>(a.q + (int64_t)row * a.pitch + t);
         const uint32_t s = a.scale[(int64_t)b * a.scale_pitch + row];
         const float factor = __builtin_bit_cast(float, s == 255u ? 0x7fc00000u : s << 23);
-        T v[8];
+        k8_any<T, 8> v;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             float f = (float)(int8_t)((i < 4 ? q.x : q.y) >> (8 * (i & 3))) * factor;

@@ -25,8 +25,6 @@ namespace {
 
 using namespace ppc;
 
-constexpr int kProjectWaves = 8;
-
 struct Range {
     uintptr_t from = 0, to = 0;
     Range(const void* p, int64_t bytes) : from(reinterpret_cast<uintptr_t>(p)), to(from + (uintptr_t)bytes) {}
@@ -53,12 +51,13 @@ pp_status_t plan_fits(const pp_adapter_bank_t* b, const pp_block_gemm_plan_t* pl
 // ---- launches (everything has been checked) ----
 
 template <typename T, int FT, int RG, bool GATED> void project_as(const K8Project& a, dim3 grid, hipStream_t stream) {
-    hipLaunchKernelGGL((k8_project<T, FT, RG, kProjectWaves, GATED>), grid, dim3(64 * kProjectWaves), 0, stream, a);
+    hipLaunchKernelGGL((k8_project<T, FT, RG, GATED>), grid, dim3(64 * kProjectWaves), 0, stream, a);
 }
 template <typename T, int FT, bool GATED> void project_rg(const K8Project& a, dim3 grid, hipStream_t stream) {
+    constexpr int most = sizeof(T) == 4 && FT == 4 ? 2 : 4;      // rank tiles in registers at a time: four would spill there
     if (a.rank_pad <= 16) project_as<T, FT, 1, GATED>(a, grid, stream);
     else if (a.rank_pad <= 32) project_as<T, FT, 2, GATED>(a, grid, stream);
-    else project_as<T, FT, 4, GATED>(a, grid, stream);
+    else project_as<T, FT, most, GATED>(a, grid, stream);
 }
 template <typename T, bool GATED> void project_ft(int ft, const K8Project& a, dim3 grid, hipStream_t stream) {
     if (ft == 1) project_rg<T, 1, GATED>(a, grid, stream);
@@ -66,12 +65,17 @@ template <typename T, bool GATED> void project_ft(int ft, const K8Project& a, di
     else project_rg<T, 4, GATED>(a, grid, stream);
 }
 
+// where the sums of what a projection left start
+float* sums_of(void* state, int n) { return reinterpret_cast<float*>(static_cast<KxToken*>(state) + n); }
+const float* sums_of(const void* state, int n) { return reinterpret_cast<const float*>(static_cast<const KxToken*>(state) + n); }
+
 // u = A x (of_a) or v = B^T x
 void launch_project(const pp_adapter_bank_t* b, bool of_a, const void* x, const void* gate, void* g, const int32_t* slot_of, void* u, int n, hipStream_t stream) {
     K8Project a{};
     a.rows = of_a ? b->k : b->m;
-    const ProjectShape sh = project_shape(a.rows, n);
-    a.x = x, a.gate = static_cast<const int8_t*>(gate), a.g = g, a.u = static_cast<float*>(u), a.slot_of = slot_of, a.rank = b->rank;
+    const ProjectShape sh = project_shape(a.rows, n, !of_a);
+    a.x = x, a.gate = static_cast<const int8_t*>(gate), a.g = g, a.slot_of = slot_of, a.rank = b->rank, a.scale = b->scale;
+    a.tokens = static_cast<KxToken*>(u), a.u = sums_of(u, n);
     a.operands = of_a ? b->a_project : b->b_project;
     a.slot_elems = (of_a ? b->a_project_slot : b->b_project_slot) / elem(b);
     a.gate_pitch = act8_pitch(n);
@@ -87,35 +91,36 @@ void launch_project(const pp_adapter_bank_t* b, bool of_a, const void* x, const 
 }
 
 // y = act(W x + bias + c B u) with the plan's W, bias and act (of_b), or with A^T in place of B
-pp_status_t launch_product(const pp_adapter_bank_t* b, bool of_b, const pp_block_gemm_plan_t* plan, const void* x, const int32_t* slot_of, const void* u, void* y,
-                           int n, hipStream_t stream) {
+pp_status_t launch_product(const pp_adapter_bank_t* b, bool of_b, const pp_block_gemm_plan_t* plan, const void* x, const void* u, void* y, int n,
+                           hipStream_t stream) {
     const int rows_in = of_b ? b->k : b->m;
-    const int splits = project_shape(rows_in, n).splits;
+    const int splits = project_shape(rows_in, n, !of_b).splits;
     const int64_t split_elems = (int64_t)n * b->rank_pad;
     if (b->dtype == PP_F16) {
         K4Expand e{};
-        e.u = static_cast<const float*>(u), e.slot_of = slot_of, e.rank = b->rank, e.scale = b->scale;
+        e.tokens = static_cast<const KxToken*>(u), e.u = sums_of(u, n);
         e.operands = of_b ? b->b_expand : b->a_expand;
         e.slot_bytes = of_b ? b->b_expand_slot : b->a_expand_slot;
         e.split_elems = split_elems;
-        e.slots = b->slots, e.splits = splits, e.rank_pad = b->rank_pad;
+        e.splits = splits, e.rank_pad = b->rank_pad;
         return block_launch_adapted(plan, x, y, n, e, stream);
     }
     const pp_status_t st = block_launch_linear_f32(plan, x, y, n, stream);
     if (st != PP_OK) return st;
     K8Expand a{};
-    a.y = static_cast<float*>(y), a.u = static_cast<const float*>(u), a.slot_of = slot_of, a.rank = b->rank, a.scale = b->scale;
+    a.y = static_cast<float*>(y), a.tokens = static_cast<const KxToken*>(u), a.u = sums_of(u, n);
     a.operands = reinterpret_cast<const float*>(of_b ? b->b_expand : b->a_expand);
     a.slot_elems = (of_b ? b->b_expand_slot : b->a_expand_slot) / 4;
     a.split_elems = split_elems;
-    a.m = of_b ? b->m : b->k, a.n = n, a.slots = b->slots, a.splits = splits, a.rank_pad = b->rank_pad, a.relu = block_plan_facts(plan).relu;
+    a.m = of_b ? b->m : b->k, a.n = n, a.splits = splits, a.rank_pad = b->rank_pad, a.relu = block_plan_facts(plan).relu;
     hipLaunchKernelGGL(k8_expand_f32, dim3((unsigned)(((int64_t)a.m + 63) / 64), (unsigned)((n + 63) / 64)), dim3(256), 0, stream, a);
     return PP_OK;
 }
 
-template <typename T, bool HELD8> void launch_grad(const K8Grad& a, dim3 grid, hipStream_t stream) {
-    if (a.rank_pad <= 16) hipLaunchKernelGGL((k8_grad<T, 1, 4, HELD8>), grid, dim3(256), 0, stream, a);
-    else if (a.rank_pad <= 32) hipLaunchKernelGGL((k8_grad<T, 2, 2, HELD8>), grid, dim3(256), 0, stream, a);
+template <typename T, bool HELD8> void launch_grad(int rw, const K8Grad& a, dim3 grid, hipStream_t stream) {
+    if (a.rank_pad <= 16) hipLaunchKernelGGL((k8_grad<T, 1, 1, HELD8>), grid, dim3(256), 0, stream, a);
+    else if (a.rank_pad <= 32) hipLaunchKernelGGL((k8_grad<T, 2, 1, HELD8>), grid, dim3(256), 0, stream, a);
+    else if (rw == 1) hipLaunchKernelGGL((k8_grad<T, 4, 1, HELD8>), grid, dim3(256), 0, stream, a);
     else hipLaunchKernelGGL((k8_grad<T, 4, 2, HELD8>), grid, dim3(256), 0, stream, a);
 }
 
@@ -191,10 +196,10 @@ pp_status_t pp_adapter_load(pp_adapter_bank_t* bank, int32_t slot, int32_t rank,
     return launched();
 }
 
-int64_t pp_adapter_u_bytes(const pp_adapter_bank_t* bank, int32_t n) { return bank && tokens_ok(bank, n) ? adapter_state_bytes(bank->k, n, bank->rank_pad) : 0; }
-int64_t pp_adapter_v_bytes(const pp_adapter_bank_t* bank, int32_t n) { return bank && tokens_ok(bank, n) ? adapter_state_bytes(bank->m, n, bank->rank_pad) : 0; }
+int64_t pp_adapter_u_bytes(const pp_adapter_bank_t* bank, int32_t n) { return bank && tokens_ok(bank, n) ? adapter_state_bytes(bank->k, n, bank->rank_pad, false) : 0; }
+int64_t pp_adapter_v_bytes(const pp_adapter_bank_t* bank, int32_t n) { return bank && tokens_ok(bank, n) ? adapter_state_bytes(bank->m, n, bank->rank_pad, true) : 0; }
 int64_t pp_adapter_work_bytes(const pp_adapter_bank_t* bank, int32_t n, int32_t count) {
-    return bank && tokens_ok(bank, n) && count >= 1 && count <= 65535 ? adapter_work_bytes(bank->m, bank->k, n, count, bank->rank_pad) : 0;
+    return bank && tokens_ok(bank, n) && count >= 1 && count <= 65535 ? grad_work(bank->m, bank->k, n, count, bank->rank_pad, bank->dtype == PP_F16).bytes : 0;
 }
 
 pp_status_t pp_adapter_project(const pp_adapter_bank_t* bank, const void* x_dev, const int32_t* slot_of_dev, void* u_dev, int32_t n, void* hip_stream) {
@@ -226,7 +231,7 @@ pp_status_t pp_adapter_run(const pp_adapter_bank_t* bank, const pp_block_gemm_pl
     launch_project(bank, true, x_dev, nullptr, nullptr, slot_of_dev, u_dev, n, stream);
     st = launched();
     if (st != PP_OK) return st;
-    st = launch_product(bank, true, plan, x_dev, slot_of_dev, u_dev, y_dev, n, stream);
+    st = launch_product(bank, true, plan, x_dev, u_dev, y_dev, n, stream);
     return st == PP_OK ? launched() : st;
 }
 
@@ -258,7 +263,7 @@ pp_status_t pp_adapter_grad_input(const pp_adapter_bank_t* bank, const pp_block_
     launch_project(bank, false, dy_dev, gate_dev, g_dev, slot_of_dev, v_dev, n, stream);
     st = launched();
     if (st != PP_OK || !dx_dev) return st;
-    st = launch_product(bank, false, plan_t, gate_dev ? g_dev : dy_dev, slot_of_dev, v_dev, dx_dev, n, stream);
+    st = launch_product(bank, false, plan_t, gate_dev ? g_dev : dy_dev, v_dev, dx_dev, n, stream);
     return st == PP_OK ? launched() : st;
 }
 
@@ -283,30 +288,44 @@ pp_status_t pp_adapter_grad_weights(const pp_adapter_bank_t* bank, const void* x
     }
     const pp_status_t st = ready(bank);
     if (st != PP_OK) return st;
-    const GradShape sh = grad_shape(bank->m, bank->k, n, count, bank->rank_pad);
-    K8Grad a{};
-    a.x = x_dev, a.g = g_dev, a.v = static_cast<const float*>(v_dev), a.u = static_cast<const float*>(u_dev);
-    a.x_pitch = act8_pitch(n), a.x_scale_pitch = act8_scale_pitch(bank->k);
-    a.x_scale = x_is_act8 ? static_cast<const uint8_t*>(x_dev) + bank->k * a.x_pitch : nullptr;
-    a.slot_of = slot_of_dev, a.which = which_dev, a.rank = bank->rank, a.scale = bank->scale;
-    a.da = da_dev, a.db = db_dev, a.work = static_cast<float*>(work_dev);
-    a.m = bank->m, a.k = bank->k, a.n = n, a.slots = bank->slots, a.rank_pad = bank->rank_pad, a.max_rank = bank->max_rank;
-    a.tiles_k = sh.tiles_k, a.count = count, a.splits = sh.splits;
-    a.u_splits = project_shape(bank->k, n).splits, a.v_splits = project_shape(bank->m, n).splits;
+    const bool half = bank->dtype == PP_F16;
+    const GradShape sh = grad_shape(bank->m, bank->k, n, count, bank->rank_pad, half);
+    const GradWork at = grad_work(bank->m, bank->k, n, count, bank->rank_pad, half);
+    char* work = static_cast<char*>(work_dev);
+    K8Turned turned;
+    turned.slots = reinterpret_cast<K8Slot*>(work), turned.masks = reinterpret_cast<K8Mask*>(work + at.masks);
+    turned.w = work + at.w, turned.down = reinterpret_cast<float*>(work + at.down);
     (void)hipGetLastError();
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    K8Turn t{};
+    t.out = turned;
+    t.w[0] = sums_of(v_dev, n), t.w[1] = sums_of(u_dev, n);
+    t.splits[0] = project_shape(bank->m, n, true).splits, t.splits[1] = project_shape(bank->k, n, false).splits;
+    t.slot_of = slot_of_dev, t.which = which_dev, t.rank = bank->rank, t.scale = bank->scale;
+    t.n = n, t.slots = bank->slots, t.blocks = (n + kAct8Block - 1) / kAct8Block, t.rank_pad = bank->rank_pad;
+    const dim3 turns((unsigned)t.blocks, (unsigned)count, (unsigned)(2 * (bank->rank_pad / 16)));
+    if (half) hipLaunchKernelGGL(k8_turn<_Float16>, turns, dim3(256), 0, stream, t);
+    else hipLaunchKernelGGL(k8_turn<float>, turns, dim3(256), 0, stream, t);
+    K8Grad a{};
+    a.in = turned;
+    a.x = x_dev, a.g = g_dev;
+    a.x_pitch = act8_pitch(n), a.x_scale_pitch = act8_scale_pitch(bank->k);
+    a.x_scale = x_is_act8 ? static_cast<const uint8_t*>(x_dev) + bank->k * a.x_pitch : nullptr;
+    a.da = da_dev, a.db = db_dev, a.work = reinterpret_cast<float*>(work + at.sums);
+    a.m = bank->m, a.k = bank->k, a.n = n, a.blocks = t.blocks, a.rank_pad = bank->rank_pad, a.max_rank = bank->max_rank;
+    a.tiles_k = sh.tiles_k, a.count = count, a.splits = sh.splits;
     const dim3 grid((unsigned)(sh.tiles_k + sh.tiles_m), (unsigned)count, (unsigned)sh.splits);
-    if (bank->dtype == PP_F16) {
-        if (x_is_act8) launch_grad<_Float16, true>(a, grid, stream);
-        else launch_grad<_Float16, false>(a, grid, stream);
+    if (half) {
+        if (x_is_act8) launch_grad<_Float16, true>(sh.rw, a, grid, stream);
+        else launch_grad<_Float16, false>(sh.rw, a, grid, stream);
     } else {
-        if (x_is_act8) launch_grad<float, true>(a, grid, stream);
-        else launch_grad<float, false>(a, grid, stream);
+        if (x_is_act8) launch_grad<float, true>(sh.rw, a, grid, stream);
+        else launch_grad<float, false>(sh.rw, a, grid, stream);
     }
     if (sh.splits > 1) {
         K8Join j{};
-        j.work = a.work, j.which = which_dev, j.rank = bank->rank, j.scale = bank->scale, j.da = da_dev, j.db = db_dev;
-        j.m = bank->m, j.k = bank->k, j.slots = bank->slots, j.rank_pad = bank->rank_pad, j.max_rank = bank->max_rank, j.count = count, j.splits = sh.splits;
+        j.slots = turned.slots, j.work = a.work, j.da = da_dev, j.db = db_dev;
+        j.m = bank->m, j.k = bank->k, j.rank_pad = bank->rank_pad, j.max_rank = bank->max_rank, j.count = count, j.splits = sh.splits;
         const int64_t wgs = (((int64_t)bank->k + bank->m) * bank->max_rank + 255) / 256;
         hipLaunchKernelGGL(k8_grad_join, dim3((unsigned)(wgs < 65536 ? wgs : 65536), (unsigned)count), dim3(256), 0, stream, j);
     }

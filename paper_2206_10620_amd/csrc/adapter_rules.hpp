@@ -25,52 +25,77 @@ inline int64_t adapter_expand_elems(int width, int rank_pad, bool half) {
     return half ? (int64_t)((width + 63) / 64) * (rank_pad / 16) * 1024 : (int64_t)width * rank_pad;
 }
 
-// A projection (u = A x): a workgroup takes 16 ft tokens, one of `splits` shares of the rows of x, whose sums are kept apart and
-// added by whoever reads u, and every `subsets`-th of the slots that its tokens name.  Splits follow from the sizes alone, since they are
-// part of u's layout.
+// A projection (u = A x, or v = B^T g): a workgroup takes 16 ft tokens and one of `splits` shares of the rows, whose sums are kept apart and
+// added by whoever reads them, and every `subsets`-th of the slots that its tokens name.  Splits follow from the sizes alone, since they
+// are part of the layout of what is left.
+//   ft: with one token to a lane a row gives 32 bytes, and many tokens ask the cache for every line four times; few tokens make few
+//   workgroups.  4096 rows, rank 16, workgroups of 8 wavefronts, 4 / 2 / 1 tokens to a lane: 4096 tokens 8.5 / 10.7 / 19.8 us, 2048
+//   7.2 / 7.0 / 8.3, 1024 7.2 / 5.9 / 5.6, 64 - / - / 5.2.
+//   splits: more shares fill the GPU, but the product that reads u does so once for every 64 rows of its own: 4096 x 4096 on 4096
+//   tokens, projection and product less the product without adapters: 2 shares 12.7 us, 4 13.3, 8 17.5 with rank 16, 19.5 and 25 with
+//   rank 32; 512 tokens 13.2 and 12.2.  v's projection may also read the gate and write g: 2 shares 104 us for all of a backward pass's
+//   first half, 4 94.
+constexpr int kProjectWaves = 8;
 struct ProjectShape {
-    int ft, waves, tiles, splits;
+    int ft, tiles, splits;
 };
-inline ProjectShape project_shape(int rows, int n) {
+inline ProjectShape project_shape(int rows, int n, bool of_v) {
     ProjectShape s;
-    s.waves = 8;
-    s.ft = n <= 256 ? 1 : (n <= 1024 ? 2 : 4);
+    s.ft = n <= 1024 ? 1 : (n <= 2048 ? 2 : 4);
     s.tiles = (n + 16 * s.ft - 1) / (16 * s.ft);
-    const int steps = (rows + 31) / 32, most = (steps + 2 * s.waves - 1) / (2 * s.waves);
-    const int want = 256 / s.tiles;
-    s.splits = want < 1 ? 1 : want;
+    s.splits = 512 / s.tiles;
+    const int steps = (rows + 31) / 32, most = (steps + 2 * kProjectWaves - 1) / (2 * kProjectWaves), limit = of_v || n <= 512 ? 4 : 2;
     if (s.splits > most) s.splits = most;
-    if (s.splits > 16) s.splits = 16;
+    if (s.splits > limit) s.splits = limit;
+    if (s.splits < 1) s.splits = 1;
     return s;
 }
+// 64 tokens with a slot of rank 16 each: 10.0 us with one subset, 7.2 with 16.
 inline int project_subsets(const ProjectShape& s, int slots) {
     int z = 512 / (s.tiles * s.splits);
     const int most = slots < 16 * s.ft ? slots : 16 * s.ft;
     if (z > most) z = most;
     return z < 1 ? 1 : z;
 }
-inline int64_t adapter_state_bytes(int rows, int n, int rank_pad) { return (int64_t)project_shape(rows, n).splits * n * rank_pad * 4; }
+// What a projection leaves: 16 bytes for each token, then the sums.
+inline int64_t adapter_state_bytes(int rows, int n, int rank_pad, bool of_v) {
+    return (int64_t)n * 16 + (int64_t)project_shape(rows, n, of_v).splits * n * rank_pad * 4;
+}
 
 // The gradients of A (k rows of x) and B (m rows of g): a workgroup takes 64 rw rows of one of them and one of `splits` shares of the
-// blocks of 128 tokens.
+// blocks of 128 tokens.  Shares fill the GPU but cost a launch that joins them, 4 us.  4096 + 4096 rows, 4096 tokens, one slot: 1 share
+// of rw 1 - us, 2 33.8, 4 25.7, 8 28.7; 512 tokens 9.6, 10.9, 11.8, -.  1024 + 4096 rows, 2000 tokens of six slots of rank 64: 24.0, 30.9,
+// 33.3, 43.8.  Rank 64 is read from the cache once for every 16 rw rows, so long sums take rw 2: 34.9 us against 39.5.
 struct GradShape {
     int rw, tiles_k, tiles_m, splits;
 };
-inline GradShape grad_shape(int m, int k, int n, int count, int rank_pad) {
+inline GradShape grad_shape(int m, int k, int n, int count, int rank_pad, bool half) {
     GradShape s;
-    s.rw = rank_pad <= 16 ? 4 : 2;
+    const int64_t blocks = (n + kAct8Block - 1) / kAct8Block, each = (blocks + count - 1) / count;      // a slot's, if they are alike
+    s.rw = rank_pad > 32 && each >= 16 ? 2 : 1;
     s.tiles_k = (k + 64 * s.rw - 1) / (64 * s.rw);
     s.tiles_m = (m + 64 * s.rw - 1) / (64 * s.rw);
-    const int64_t blocks = (n + kAct8Block - 1) / kAct8Block, wgs = (int64_t)(s.tiles_k + s.tiles_m) * count;
-    int64_t w = 512 / wgs;
-    if (w > blocks) w = blocks;
-    if (w > 16) w = 16;
+    const int64_t wgs = (int64_t)(s.tiles_k + s.tiles_m) * count;
+    int64_t w = each <= (half ? 4 : 1) ? 1 : 512 / wgs;
+    if (w > each) w = each;
+    if (w > 8) w = 8;
     s.splits = w < 1 ? 1 : (int)w;
     return s;
 }
-inline int64_t adapter_work_bytes(int m, int k, int n, int count, int rank_pad) {
-    const GradShape s = grad_shape(m, k, n, count, rank_pad);
-    return s.splits == 1 ? 16 : (int64_t)s.splits * count * ((int64_t)m + k) * rank_pad * 4;
+// Scratch memory of the gradients: offsets in bytes, multiples of 16.
+struct GradWork {
+    int64_t masks, w, down, sums, bytes;
+};
+inline GradWork grad_work(int m, int k, int n, int count, int rank_pad, bool half) {
+    const int64_t blocks = (n + kAct8Block - 1) / kAct8Block;
+    const GradShape s = grad_shape(m, k, n, count, rank_pad, half);
+    GradWork o;
+    o.masks = (int64_t)count * 16;
+    o.w = o.masks + count * blocks * 16;
+    o.down = o.w + count * 2 * blocks * rank_pad * kAct8Block * 4;       // two binary16 parts or one binary32
+    o.sums = o.down + (half ? count * 2 * blocks * rank_pad * 4 : 0);
+    o.bytes = o.sums + (s.splits > 1 ? (int64_t)s.splits * count * ((int64_t)m + k) * rank_pad * 4 : 0);
+    return o;
 }
 
 }  // namespace ppc

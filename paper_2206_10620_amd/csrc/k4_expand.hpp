@@ -16,19 +16,32 @@
 
 namespace ppc {
 
+// What a token has: the projection leaves it for whoever reads u, which saves them a load that waits for another.
+struct KxToken {
+    int32_t slot;               // -1: no adapter
+    int32_t rank;               // 0 for none
+    float factor;
+    int32_t unused;
+};
+
 struct K4Expand {
+    const KxToken* tokens;      // [n]
     const float* u;             // [splits][n][rank_pad]
-    const int32_t* slot_of;     // [n]
-    const int32_t* rank;        // [slots]
-    const float* scale;         // [slots]
     const void* operands;       // [slot][64-row tile][rank_pad / 16][2][64 lanes][8] binary16
     int64_t slot_bytes, split_elems;
-    int32_t slots, splits, rank_pad;
+    int32_t splits, rank_pad;
 };
 
 typedef _Float16 kx_h8 __attribute__((ext_vector_type(8)));
 typedef float kx_f4 __attribute__((ext_vector_type(4)));
 typedef float kx_f16 __attribute__((ext_vector_type(16)));
+
+// v = hi + lo up to 2^-22 of v (or 2^-25 absolute); an infinity or a NaN is hi alone
+__device__ __forceinline__ void kx_parts(float v, _Float16& hi, _Float16& lo) {
+    hi = (_Float16)v;
+    const float rest = v - (float)hi;
+    lo = __builtin_fabsf(v) <= 65504.0f ? (_Float16)rest : (_Float16)0.0f;
+}
 
 // The power of two that brings the largest finite magnitude (its bits) of a token's u to [2^14, 2^15); 2^126 at most, so that
 // its inverse is a normal number.
@@ -38,22 +51,55 @@ __device__ __forceinline__ int kx_shift(uint32_t top_bits) {
 }
 __device__ __forceinline__ float kx_pow2(int e) { return __builtin_bit_cast(float, (uint32_t)(127 + e) << 23); }
 
-// v = hi + lo up to 2^-22 of v (or 2^-25 absolute); an infinity or a NaN is hi alone
-__device__ __forceinline__ void kx_parts(float v, _Float16& hi, _Float16& lo) {
-    hi = (_Float16)v;
-    const float rest = v - (float)hi;
-    lo = __builtin_fabsf(v) <= 65504.0f ? (_Float16)rest : (_Float16)0.0f;
+typedef __fp16 kx_p2 __attribute__((ext_vector_type(2)));
+typedef _Float16 kx_h2 __attribute__((ext_vector_type(2)));
+
+// Eight fp32 values as two binary16 parts, v * 2^shift = hi + lo up to 2^-21 of it (or 2^-24 of the token's largest), and the
+// factor that undoes the shift.  Both parts are cut, not rounded: what hi leaves, lo takes.  A lane holds half of its token's values,
+// lane ^ 32 the other.  An infinity or a NaN is hi alone, and the shift that of the token's other values.
+template <int G> __device__ __forceinline__ void kx_split(const float (&v)[G][8], kx_h8 (&hi)[G], kx_h8 (&lo)[G], float& down) {
+    float top = 0.0f;
+#pragma unroll
+    for (int c = 0; c < G; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = __builtin_fmaxf(top, __builtin_fabsf(v[c][i]));
+    top = __builtin_fmaxf(top, __shfl_xor(top, 32));
+    const bool odd = __builtin_amdgcn_ballot_w64(top > 3.4028235e38f) != 0;   // an infinity somewhere: rare
+    if (odd) {
+        top = 0.0f;
+#pragma unroll
+        for (int c = 0; c < G; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float m = __builtin_fabsf(v[c][i]);
+                top = m <= 3.4028235e38f && m > top ? m : top;
+            }
+        top = __builtin_fmaxf(top, __shfl_xor(top, 32));
+    }
+    const int shift = kx_shift(__builtin_bit_cast(uint32_t, top));
+    const float up = kx_pow2(shift);
+    down = kx_pow2(-shift);
+#pragma unroll
+    for (int c = 0; c < G; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            const float a = v[c][i] * up, b = v[c][i + 1] * up;
+            const kx_h2 h = __builtin_bit_cast(kx_h2, __builtin_amdgcn_cvt_pkrtz(a, b));
+            const kx_h2 l = __builtin_bit_cast(kx_h2, __builtin_amdgcn_cvt_pkrtz(a - (float)h.x, b - (float)h.y));
+            hi[c][i] = h.x, hi[c][i + 1] = h.y;
+            lo[c][i] = l.x, lo[c][i + 1] = l.y;
+        }
+    if (odd) {                                                                // an infinity leaves itself less itself, no number
+#pragma unroll
+        for (int c = 0; c < G; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) lo[c][i] = __builtin_fabsf(v[c][i]) <= 3.4028235e38f ? lo[c][i] : (_Float16)0.0f;
+    }
 }
 
-// The slot that a token's entry stands for: -1 for none.
-__device__ __forceinline__ int kx_slot(const int32_t* slot_of, const int32_t* rank, int slots, int token, int n) {
-    if (token >= n) return -1;
-    const int s = slot_of[token];
-    return (uint32_t)s < (uint32_t)slots && rank[s] > 0 ? s : -1;
-}
-
-// The slot of the first token that is left (sl < 0: none, or taken already); -1 if none is.
-template <int N> __device__ __forceinline__ int kx_next(const int (&sl)[N]) {
+// The next slot: that of the first token left (sl < 0: none, or taken already), which it takes with all others of the slot;
+// sel: whose they are.  -1 and nobody's if no token is left.
+template <int N> __device__ __forceinline__ int kx_take(int (&sl)[N], bool (&sel)[N]) {
     int s = -1;
 #pragma unroll
     for (int i = N - 1; i >= 0; --i) {
@@ -61,77 +107,172 @@ template <int N> __device__ __forceinline__ int kx_next(const int (&sl)[N]) {
         const int first = __builtin_amdgcn_readlane(sl[i], left ? (int)__builtin_ctzll(left) : 0);
         s = left ? first : s;
     }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        sel[i] = s >= 0 && sl[i] == s;
+        sl[i] = sel[i] ? -1 : sl[i];
+    }
     return s;
 }
 
-// Adds to acc (two 32-row tiles of row tile rt by NT tiles of 32 columns from col0) the adapters' part of every `parts`-th
-// slot from `part` on.
-template <int NT>
-__device__ __forceinline__ void k4_expand(const K4Expand& e, kx_f16 (&acc)[2][NT], int col0, int n, int rt, int lane, int part, int parts) {
-    int sl[NT];
+__device__ __forceinline__ KxToken kx_token(const int32_t* slot_of, const int32_t* rank, const float* scale, int slots, int token, int n) {
+    KxToken k = {-1, 0, 0.0f, 0};
+    const int s = token < n ? slot_of[token] : -1;
+    if ((uint32_t)s < (uint32_t)slots) k.rank = rank[s], k.factor = scale[s];
+    k.slot = k.rank > 0 ? s : -1;
+    return k;
+}
+
+// The first lane of every slot among lanes 0 .. 31 (slot < 0: none), as a mask.
+__device__ __forceinline__ uint32_t kx_leaders(int slot) {
+    const uint32_t valid = (uint32_t)__builtin_amdgcn_ballot_w64(slot >= 0);
+    if (valid == 0) return 0;
+    const int s0 = __builtin_amdgcn_readlane(slot, __builtin_ctz(valid));
+    if ((uint32_t)__builtin_amdgcn_ballot_w64(slot == s0) == valid) return valid & (0u - valid);
+    uint32_t later = 0;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) sl[nt] = kx_slot(e.slot_of, e.rank, e.slots, col0 + nt * 32 + (lane & 31), n);
-    int index = 0;
-    for (;;) {
-        const int s = kx_next(sl);
-        if (s < 0) break;
-        const bool mine = parts == 1 || index % parts == part;
-        ++index;
-        const int chunks = mine ? (__builtin_amdgcn_readfirstlane(e.rank[s]) + 15) / 16 : 0;
-        const float factor = e.scale[s];
-        const unsigned char* ops = static_cast<const unsigned char*>(e.operands) + s * e.slot_bytes + (int64_t)rt * (e.rank_pad / 16) * 2048 + lane * 16;
+    for (int i = 0; i < 31; ++i) later |= (uint32_t)__builtin_amdgcn_ballot_w64(slot == __builtin_amdgcn_readlane(slot, i)) & (~1u << i);
+    return valid & ~later;
+}
+
+// The adapters' part of a wavefront's product, 32 columns and 16 ranks at a time.
+template <int NT> struct KxItems {
+    const K4Expand& e;
+    int t0, n;
+    const float* u0;
+    const unsigned char* ops0;
+
+    // u of tile nt, ranks from 16 c on; unwritten memory where a token has no adapter or a lower rank
+    __device__ __forceinline__ void load(int nt, int c, float (&v)[1][8]) const {
+        constexpr int B = NT == 1 ? 4 : (NT == 2 ? 2 : 1);      // shares in flight at a time
+        for (int s0 = 0; s0 < e.splits; s0 += B) {
+            kx_f4 w[B][2];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const bool sel = sl[nt] == s;
-            if (sel) sl[nt] = -1;
-            if (chunks == 0 || __builtin_amdgcn_ballot_w64(sel) == 0) continue;
-            const float* up = e.u + (int64_t)(col0 + nt * 32 + (lane & 31)) * e.rank_pad + 8 * (lane >> 5);
-            auto fetch = [&](int c, float (&v)[8]) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-                if (sel)
-                    for (int sp = 0; sp < e.splits; ++sp) {
-                        const kx_f4* p = reinterpret_cast<const kx_f4*>(up + sp * e.split_elems + c * 16);
-                        const kx_f4 a = p[0], b = p[1];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) v[i] += a[i], v[4 + i] += b[i];
-                    }
-            };
-            float v[8];
-            uint32_t top = 0;
-            for (int c = chunks - 1; c >= 0; --c) {                 // ends on chunk 0, which stays in v
-                fetch(c, v);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t b = __builtin_bit_cast(uint32_t, v[i]) & 0x7fffffffu;
-                    if (b < 0x7f800000u && b > top) top = b;
+            for (int b = 0; b < B; ++b) {
+                w[b][0] = kx_f4(0.0f), w[b][1] = kx_f4(0.0f);
+                if (s0 + b < e.splits && c * 16 < e.rank_pad && t0 + nt * 32 < n) {
+                    const kx_f4* p = reinterpret_cast<const kx_f4*>(u0 + (s0 + b) * e.split_elems + (int64_t)(nt * 32) * e.rank_pad + c * 16);
+                    w[b][0] = p[0], w[b][1] = p[1];
                 }
             }
-            const uint32_t other = (uint32_t)__shfl_xor((int)top, 32);
-            top = top > other ? top : other;
-            const int shift = kx_shift(top);
-            const float up2 = kx_pow2(shift), down2 = kx_pow2(-shift);
-            kx_f16 t[2] = {kx_f16(0.0f), kx_f16(0.0f)};
-            for (int c = 0; c < chunks; ++c) {
-                if (c) fetch(c, v);
-                kx_h8 hi, lo;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    _Float16 h, l;
-                    kx_parts(v[i] * up2, h, l);
-                    hi[i] = h, lo[i] = l;
+            for (int q = 0; q < 8; ++q) {
+                float x = w[0][q >> 2][q & 3];
+#pragma unroll
+                for (int b = 1; b < B; ++b) x += w[b][q >> 2][q & 3];
+                v[0][q] = s0 ? v[0][q] + x : x;
+            }
+        }
+    }
+
+    struct Operand {
+        kx_h8 v[2];
+        int slot;               // whose it is
+    };
+
+    // Every lane splits its own token's u, whatever its slot, so that one latency serves all tokens; then the slots are gone
+    // through, D of them with their B on the way at once.  b may hold a slot's from the tile before, of the same ranks.  Of the slots
+    // (those of the leaders) every `parts`-th is this wavefront's.
+    template <int NTI, int D>
+    __device__ __forceinline__ void multiply(int c, const KxToken& tok, uint32_t leaders, int part, int parts, float (&v)[1][8], Operand (&b)[D],
+                                             kx_f16 (&acc)[2][NT]) const {
+        uint32_t left = leaders & (uint32_t)__builtin_amdgcn_ballot_w64(tok.rank > c * 16);
+        if (left == 0) return;
+        for (int i = 0; i < part; ++i) left &= left - 1;
+        if (left == 0) return;
+        bool have[D];
+        auto fetch = [&](Operand& to, bool& got) {
+            got = left != 0;
+            if (got) {
+                const int s = __builtin_amdgcn_readlane(tok.slot, __builtin_ctz(left));
+                for (int i = 0; i < parts; ++i) left &= left - 1;
+                if (to.slot != s) {
+                    const unsigned char* ops = ops0 + s * e.slot_bytes + c * 2048;
+                    to.v[0] = *reinterpret_cast<const kx_h8*>(ops), to.v[1] = *reinterpret_cast<const kx_h8*>(ops + 1024);
+                    to.slot = s;
                 }
+            }
+        };
+#pragma unroll
+        for (int d = 0; d < D; ++d) fetch(b[d], have[d]);
+        kx_h8 hi[1], lo[1];
+        float down;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[0][q] = tok.rank > c * 16 ? v[0][q] : 0.0f;             // (not written there)
+        kx_split<1>(v, hi, lo, down);
+        // the factor of the token's sums: its slot's and what undoes the shift, kept finite so that a sum of 0 stays one
+        const float f = __builtin_fminf(__builtin_fmaxf(down * tok.factor, -3.4028235e38f), 3.4028235e38f);
+#pragma unroll 1
+        while (have[0]) {
+#pragma unroll
+            for (int d = 0; d < D; ++d) {
+                if (!have[d]) continue;
+                const bool sel = tok.slot == b[d].slot;
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt) {
-                    const kx_h8 b = *reinterpret_cast<const kx_h8*>(ops + c * 2048 + mt * 1024);
-                    t[mt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(b, hi, t[mt], 0, 0, 0);
-                    t[mt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(b, lo, t[mt], 0, 0, 0);
+                    kx_f16 t = kx_f16(0.0f);
+                    t = __builtin_amdgcn_mfma_f32_32x32x16_f16(b[d].v[mt], hi[0], t, 0, 0, 0);
+                    t = __builtin_amdgcn_mfma_f32_32x32x16_f16(b[d].v[mt], lo[0], t, 0, 0, 0);
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) acc[mt][NTI][q] = sel ? __builtin_fmaf(t[q], f, acc[mt][NTI][q]) : acc[mt][NTI][q];
+                    __builtin_amdgcn_sched_barrier(0);           // one tile's sums at a time: with all of them in registers the rest would spill
                 }
             }
 #pragma unroll
-            for (int mt = 0; mt < 2; ++mt)
+            for (int d = 0; d < D; ++d) fetch(b[d], have[d]);
+        }
+    }
+};
+
+// Adds to acc (two 32-row tiles of row tile rt by NT tiles of 32 columns from col0) the adapters' part, or, of `parts` wavefronts
+// with the same columns, the part of wavefront `part`: they deal the ranks' chunks out among them first, then the slots.
+template <int NT>
+__device__ __forceinline__ void k4_expand(const K4Expand& e, kx_f16 (&acc)[2][NT], int col0, int n, int rt, int lane, int part, int parts) {
+    constexpr int D = NT == 1 ? 8 : (NT == 2 ? 4 : 1);
+    KxItems<NT> items = {e, col0 + (lane & 31), n};
+    items.u0 = e.u + (int64_t)items.t0 * e.rank_pad + 8 * (lane >> 5);
+    items.ops0 = static_cast<const unsigned char*>(e.operands) + (int64_t)rt * (e.rank_pad / 16) * 2048 + lane * 16;
+    int by_chunk = 1;
+    while (by_chunk < parts && 2 * by_chunk * 16 <= e.rank_pad) by_chunk *= 2;
+    const int by_slot = parts / by_chunk, c0 = part % by_chunk, my_slot = part / by_chunk;
+    float v[1][8], v2[1][8];
+    items.load(0, c0, v);
+    KxToken tok[NT];
+    uint32_t leaders[NT];
+    int top = 0;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[mt][nt][i] = sel ? __builtin_fmaf(t[mt][i] * down2, factor, acc[mt][nt][i]) : acc[mt][nt][i];
+    for (int nt = 0; nt < NT; ++nt) {
+        tok[nt] = KxToken{-1, 0, 0.0f, 0};
+        if (items.t0 + nt * 32 < n) tok[nt] = e.tokens[items.t0 + nt * 32];
+        top = tok[nt].rank > top ? tok[nt].rank : top;
+    }
+    if (__builtin_amdgcn_ballot_w64(top > c0 * 16) == 0) return;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) leaders[nt] = kx_leaders(tok[nt].slot);
+#pragma unroll 1
+    for (int c = c0; __builtin_amdgcn_ballot_w64(top > c * 16); c += by_chunk) {
+        typename KxItems<NT>::Operand b[D];
+#pragma unroll
+        for (int d = 0; d < D; ++d) b[d].slot = -1;
+        if constexpr (NT == 4) {
+            items.load(1, c, v2);
+            items.template multiply<0, D>(c, tok[0], leaders[0], my_slot, by_slot, v, b, acc);
+            items.load(2, c, v);
+            items.template multiply<1, D>(c, tok[1], leaders[1], my_slot, by_slot, v2, b, acc);
+            items.load(3, c, v2);
+            items.template multiply<2, D>(c, tok[2], leaders[2], my_slot, by_slot, v, b, acc);
+            items.load(0, c + by_chunk, v);
+            items.template multiply<3, D>(c, tok[3], leaders[3], my_slot, by_slot, v2, b, acc);
+        } else if constexpr (NT == 2) {
+            items.load(1, c, v2);
+            items.template multiply<0, D>(c, tok[0], leaders[0], my_slot, by_slot, v, b, acc);
+            items.load(0, c + by_chunk, v);
+            items.template multiply<1, D>(c, tok[1], leaders[1], my_slot, by_slot, v2, b, acc);
+        } else {
+            items.load(0, c + by_chunk, v2);
+            items.template multiply<0, D>(c, tok[0], leaders[0], my_slot, by_slot, v, b, acc);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[0][q] = v2[0][q];
         }
     }
 }

@@ -7,6 +7,7 @@
 #include <cstdint>
 #include <type_traits>
 
+#include "adapter_rules.hpp"
 #include "k4_expand.hpp"
 #include "pieces.hpp"
 
@@ -110,17 +111,18 @@ struct K8Project {
     const void* x;              // [rows][n]
     const int8_t* gate;         // [rows][gate_pitch]
     void* g;                    // [rows][n]
+    KxToken* tokens;            // [n]
     float* u;                   // [splits][n][rank_pad]
     const int32_t* slot_of;
     const int32_t* rank;
+    const float* scale;
     const void* operands;       // [slot][rank tile][steps][64 lanes][8]
     int64_t slot_elems, gate_pitch;
     int32_t rows, n, steps, slots, rank_pad, splits;
 };
-constexpr int k8_project_lds(int ft, int waves) { return waves * ft * 64 * 16; }
-
-template <typename T, int FT, int RG, int W, bool GATED>
-__global__ __launch_bounds__(64 * W) void k8_project(const K8Project a) {
+template <typename T, int FT, int RG, bool GATED>
+__global__ __launch_bounds__(64 * kProjectWaves) void k8_project(const K8Project a) {
+    constexpr int W = kProjectWaves;
     __shared__ k8_f4 red[W * FT * 64];
     const int lane = (int)(threadIdx.x & 63u), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int c = lane & 15, g = lane >> 4;
@@ -132,50 +134,57 @@ __global__ __launch_bounds__(64 * W) void k8_project(const K8Project a) {
     const T* x = static_cast<const T*>(a.x);
     float* u = a.u + (int64_t)split * a.n * a.rank_pad;
 
+    typedef k8_any<T, FT> Piece;
+    auto load = [&](int st, Piece (&v)[8], bool write_g) {
+        const int row0 = st * 32 + g * 8;
+        const T* src = x + (int64_t)row0 * a.n + mine0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = k8_load<T, FT>(src + (int64_t)i * a.n, row0 + i < a.rows ? left : 0);
+        if constexpr (GATED) {
+            k8_any<int8_t, FT> q[8];
+            const int8_t* gate = a.gate + (int64_t)row0 * a.gate_pitch + mine0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[i] = k8_load<int8_t, FT>(gate + i * a.gate_pitch, row0 + i < a.rows && left > 0 ? FT : 0);
+            T* dst = static_cast<T*>(a.g) + (int64_t)row0 * a.n + mine0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+#pragma unroll
+                for (int f = 0; f < FT; ++f)
+                    if (!(k8_at<k8_any<int8_t, FT>, int8_t>(q[i], f) > 0)) k8_put(v[i], f, (T)0.0f);
+                if (write_g && row0 + i < a.rows) k8_store<T, FT>(dst + (int64_t)i * a.n, left, v[i]);
+            }
+        }
+    };
+
     // One slot's tokens (slot -1: only the gate), ranks from tile rt0 on.
-    auto pass = [&](int slot, int rt0, int tiles, bool write_g) {
+    auto pass = [&](int slot, int rt0, int tiles, bool is_first) {
         k8_f4 acc[RG][FT];
 #pragma unroll
         for (int r = 0; r < RG; ++r)
 #pragma unroll
             for (int f = 0; f < FT; ++f) acc[r][f] = k8_f4(0.0f);
+        const bool write_g = GATED && is_first && blockIdx.y == 0;
         const T* ops = static_cast<const T*>(a.operands) + (slot < 0 ? 0 : slot * a.slot_elems) + (int64_t)rt0 * a.steps * 512 + lane * 8;
-        auto load = [&](int st, T (&v)[8][FT]) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int row = st * 32 + g * 8 + i;
-                k8_load<T, FT>(x + (int64_t)row * a.n + mine0, row < a.rows ? left : 0, v[i]);
-            }
-            if constexpr (GATED) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int row = st * 32 + g * 8 + i;
-                    if (row < a.rows && left > 0) {
-                        int8_t q[FT];
-                        k8_load<int8_t, FT>(a.gate + (int64_t)row * a.gate_pitch + mine0, FT, q);
-#pragma unroll
-                        for (int f = 0; f < FT; ++f) v[i][f] = q[f] > 0 ? v[i][f] : (T)0.0f;
-                        if (write_g) k8_store<T, FT>(static_cast<T*>(a.g) + (int64_t)row * a.n + mine0, left, v[i]);
-                    }
-                }
-            }
-        };
-#pragma unroll 2
+        Piece v[8];
+        if (w0 < w1) load(w0, v, write_g);
         for (int st = w0; st < w1; ++st) {
-            T v[8][FT];
-            load(st, v);
+            Piece next[8];
+            k8_v8<T> op[RG];
 #pragma unroll
             for (int r = 0; r < RG; ++r)
-                if (r < tiles) {
-                    const k8_v8<T> op = *reinterpret_cast<const k8_v8<T>*>(ops + ((int64_t)r * a.steps + st) * 512);
+                if (r < tiles) op[r] = *reinterpret_cast<const k8_v8<T>*>(ops + ((int64_t)r * a.steps + st) * 512);
+            if (st + 1 < w1) load(st + 1, next, write_g);
 #pragma unroll
-                    for (int f = 0; f < FT; ++f) {
-                        k8_v8<T> b;
+            for (int f = 0; f < FT; ++f) {
+                k8_v8<T> b;
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) b[i] = v[i][f];
-                        acc[r][f] = k8_mfma(op, b, acc[r][f]);
-                    }
-                }
+                for (int i = 0; i < 8; ++i) b[i] = k8_at<Piece, T>(v[i], f);
+#pragma unroll
+                for (int r = 0; r < RG; ++r)
+                    if (r < tiles) acc[r][f] = k8_mfma(op[r], b, acc[r][f]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = next[i];
         }
         if (slot < 0) return;
         const int rank = a.rank[slot];
@@ -189,7 +198,7 @@ __global__ __launch_bounds__(64 * W) void k8_project(const K8Project a) {
                 for (int i = (int)threadIdx.x; i < FT * 64; i += 64 * W) {
                     const int f = i >> 6, ln = i & 63, t = t0 + (ln & 15) * FT + f, j = (rt0 + r) * 16 + (ln >> 4) * 4;
                     k8_f4 v = red[i];
-#pragma unroll
+#pragma unroll 4
                     for (int w = 1; w < W; ++w) v += red[w * FT * 64 + i];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) v[e] = j + e < rank ? v[e] : 0.0f;
@@ -200,22 +209,36 @@ __global__ __launch_bounds__(64 * W) void k8_project(const K8Project a) {
     };
 
     int sl[FT];
+    bool sel[FT];
 #pragma unroll
-    for (int f = 0; f < FT; ++f) sl[f] = kx_slot(a.slot_of, a.rank, a.slots, mine0 + f, a.n);
-    bool write_g = GATED && blockIdx.y == 0;
-    for (int index = 0;; ++index) {
-        const int s = kx_next(sl);
-        if (s < 0) break;
-#pragma unroll
-        for (int f = 0; f < FT; ++f) sl[f] = sl[f] == s ? -1 : sl[f];
-        if (index % (int)gridDim.y != (int)blockIdx.y) continue;
-        const int tiles = (__builtin_amdgcn_readfirstlane(a.rank[s]) + 15) / 16;
-        for (int rt0 = 0; rt0 < tiles; rt0 += RG) {
-            pass(s, rt0, tiles - rt0, write_g);
-            write_g = false;
-        }
+    for (int f = 0; f < FT; ++f) {
+        const KxToken tok = kx_token(a.slot_of, a.rank, a.scale, a.slots, mine0 + f, a.n);
+        sl[f] = tok.slot;
+        if (split == 0 && blockIdx.y == 0 && threadIdx.x < 16 && mine0 + f < a.n) a.tokens[mine0 + f] = tok;
     }
-    if (write_g) pass(-1, 0, 0, true);
+    bool is_first = true;
+    uint32_t leaders = 0;                                        // one token to a lane: the slots' first ones, from this workgroup's first on
+    if constexpr (FT == 1) {
+        leaders = kx_leaders(sl[0]);
+        for (int i = 0; i < (int)blockIdx.y; ++i) leaders &= leaders - 1;
+    }
+    for (int index = 0;; ++index) {
+        int s;
+        if constexpr (FT == 1) {
+            s = leaders ? __builtin_amdgcn_readlane(sl[0], __builtin_ctz(leaders ? leaders : 1u)) : -1;
+            for (int i = 0; i < (int)gridDim.y; ++i) leaders &= leaders - 1;
+        } else {
+            s = kx_take(sl, sel);
+        }
+        if (s < 0 && !(GATED && is_first && blockIdx.y == 0)) break;
+        if (FT > 1 && s >= 0 && index % (int)gridDim.y != (int)blockIdx.y) continue;
+        const int tiles = s < 0 ? 1 : (__builtin_amdgcn_readfirstlane(a.rank[s]) + 15) / 16;
+        for (int rt0 = 0; rt0 < tiles; rt0 += RG) {
+            pass(s, rt0, s < 0 ? 0 : tiles - rt0, is_first);
+            is_first = false;
+        }
+        if (s < 0) break;
+    }
 }
 
 // ---- expansion in binary32 ----
@@ -223,61 +246,67 @@ __global__ __launch_bounds__(64 * W) void k8_project(const K8Project a) {
 // A wavefront takes 16 rows of y and 64 tokens, four to a lane.
 struct K8Expand {
     float* y;                   // [m][n]
+    const KxToken* tokens;      // [n]
     const float* u;             // [splits][n][rank_pad]
-    const int32_t* slot_of;
-    const int32_t* rank;
-    const float* scale;
     const float* operands;      // [slot][m][rank_pad]
     int64_t slot_elems, split_elems;
-    int32_t m, n, slots, splits, rank_pad, relu;
+    int32_t m, n, splits, rank_pad, relu;
 };
 __global__ __launch_bounds__(256) void k8_expand_f32(const K8Expand a) {
     const int lane = (int)(threadIdx.x & 63u), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int c = lane & 15, g = lane >> 4;
     const int row0 = ((int)blockIdx.x * 4 + wave) * 16, t0 = (int)blockIdx.y * 64 + c * 4, left = a.n - t0;
     if (row0 >= a.m) return;
-    int sl[4];
+    KxToken tok[4];
     bool any = false;
 #pragma unroll
     for (int f = 0; f < 4; ++f) {
-        sl[f] = kx_slot(a.slot_of, a.rank, a.slots, t0 + f, a.n);
-        any = any || sl[f] >= 0;
+        tok[f] = KxToken{-1, 0, 0.0f, 0};
+        if (f < left) tok[f] = a.tokens[t0 + f];
+        any = any || tok[f].slot >= 0;
     }
+    k8_any<float, 4> y[4];                                       // [row][token]
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = k8_load<float, 4>(a.y + (int64_t)(row0 + 4 * g + i) * a.n + t0, row0 + 4 * g + i < a.m ? left : 0);
     if (!a.relu && __builtin_amdgcn_ballot_w64(any) == 0) return;
-    float y[4][4];                                               // [row][token]
+    const float* up = a.u + (int64_t)t0 * a.rank_pad + 4 * g;
+    const float* ops0 = a.operands + (int64_t)(row0 + c) * a.rank_pad + 4 * g;
+    for (int r0 = 0; r0 < a.rank_pad; r0 += 16) {
+        // every lane its own tokens' u, whatever their slots; then slot by slot
+        k8_f4 w[4];
+        for (int s0 = 0; s0 < a.splits; s0 += 4) {
+            k8_f4 v[4][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) k8_load<float, 4>(a.y + (int64_t)(row0 + 4 * g + i) * a.n + t0, row0 + 4 * g + i < a.m ? left : 0, y[i]);
-    for (;;) {
-        const int s = kx_next(sl);
-        if (s < 0) break;
-        const int tiles = (__builtin_amdgcn_readfirstlane(a.rank[s]) + 15) / 16;
-        const float factor = a.scale[s];
-        const float* ops = a.operands + s * a.slot_elems + (int64_t)(row0 + c) * a.rank_pad + 4 * g;
-        const float* up = a.u + (int64_t)t0 * a.rank_pad + 4 * g;
-        bool sel[4];
-        k8_f4 acc[4];
+            for (int b = 0; b < 4; ++b)
 #pragma unroll
-        for (int f = 0; f < 4; ++f) {
-            sel[f] = sl[f] == s;
-            if (sel[f]) sl[f] = -1;
-            acc[f] = k8_f4(0.0f);
-        }
-        for (int r = 0; r < tiles; ++r) {
-            k8_f4 op = k8_f4(0.0f);
-            if (row0 + c < a.m) op = *reinterpret_cast<const k8_f4*>(ops + r * 16);
+                for (int f = 0; f < 4; ++f) {
+                    v[b][f] = k8_f4(0.0f);
+                    if (s0 + b < a.splits && f < left) v[b][f] = *reinterpret_cast<const k8_f4*>(up + (s0 + b) * a.split_elems + (int64_t)f * a.rank_pad + r0);
+                }
 #pragma unroll
             for (int f = 0; f < 4; ++f) {
-                k8_f4 w = k8_f4(0.0f);
-                if (sel[f])
-                    for (int sp = 0; sp < a.splits; ++sp) w += *reinterpret_cast<const k8_f4*>(up + sp * a.split_elems + (int64_t)f * a.rank_pad + r * 16);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(op[i], w[i], acc[f], 0, 0, 0);
+                const k8_f4 x = v[0][f] + v[1][f] + v[2][f] + v[3][f];
+                w[f] = s0 ? w[f] + x : x;
             }
         }
+        int sl[4];
+        bool sel[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int f = 0; f < 4; ++f) sl[f] = tok[f].rank > r0 ? tok[f].slot : -1;
+        for (;;) {
+            const int s = kx_take(sl, sel);
+            if (s < 0) break;
+            k8_f4 op = k8_f4(0.0f);
+            if (row0 + c < a.m) op = *reinterpret_cast<const k8_f4*>(ops0 + s * a.slot_elems + r0);
 #pragma unroll
-            for (int f = 0; f < 4; ++f) y[i][f] = sel[f] ? __builtin_fmaf(acc[f][i], factor, y[i][f]) : y[i][f];
+            for (int f = 0; f < 4; ++f) {
+                k8_f4 acc = k8_f4(0.0f);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(op[i], w[f][i], acc, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i][f] = sel[f] ? __builtin_fmaf(acc[i], tok[f].factor, y[i][f]) : y[i][f];
+            }
+        }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -291,185 +320,272 @@ __global__ __launch_bounds__(256) void k8_expand_f32(const K8Expand a) {
 // ---- gradients of A and B ----
 // G[p][j] = c_s sum over the tokens t of slot s of z[p][t] w[t][j], with z = x and w = v for A, z = g and w = u for B.
 //
-// Both operands have the tokens, the reduction, next to each other in memory or can be had so: z's 16 bytes of a row come straight
-// from memory, w's 128 tokens are turned through LDS once for the workgroup's 64 RW rows.  In binary16 they are two parts, hi and lo,
-// after a power of two taken out for each rank and block; x in 8 bits is exact in binary16, its power of two for each row and block
-// joins the other when a block's sum is added to the whole.  Tokens of other slots in a block are taken as zeros on both sides; blocks
-// without one of the slot's are passed over.
-// A workgroup takes a share of the blocks; with several shares the sums are joined in order by k8_grad_join.
-struct K8Grad {
-    const void* x;              // [k][n], or int8 [k][x_pitch]
-    const uint8_t* x_scale;     // [block][x_scale_pitch]
-    const void* g;              // [m][n]
-    const float* v;             // [v_splits][n][rank_pad]
-    const float* u;             // [u_splits][n][rank_pad]
+// Both operands have the tokens, the reduction, next to each other: 16 bytes of a row of z come straight from memory in the order the
+// matrix instruction wants.  w is small and wanted by every 16 rows of z: k8_turn brings it into operand order once, slot by slot and block
+// of 128 tokens by block, with zeros for the tokens of other slots; blocks without one of the slot's are passed over.  In binary16 it is in
+// two parts, hi and lo, after a power of two taken out for each rank and block; x in 8 bits is exact in binary16, and its power of
+// two for each row and block joins the other when a block's sum is added to the whole.
+
+// What k8_turn leaves, for each slot listed.
+struct K8Slot {
+    int32_t rank;               // 0: nothing to do
+    float factor;
+    int32_t unused[2];
+};
+struct K8Mask {
+    uint64_t half[2];           // which of a block's 128 tokens are the slot's
+};
+struct K8Turned {
+    K8Slot* slots;              // [count]
+    K8Mask* masks;              // [count][blocks]
+    void* w;                    // [count][2: v, u][blocks][rank tile][4][parts][64 lanes][8]
+    float* down;                // [count][2][blocks][rank_pad]: undoes the power of two
+};
+template <typename T> constexpr int kK8Parts = sizeof(T) == 2 ? 2 : 1;
+
+struct K8Turn {
+    K8Turned out;
+    const KxToken* tokens;
+    const float* w[2];          // v, u: [splits][n][rank_pad]
     const int32_t* slot_of;
     const int32_t* which;
     const int32_t* rank;
     const float* scale;
+    int32_t n, slots, blocks, rank_pad, splits[2];
+};
+
+// A workgroup turns a block of a rank tile of v or u for one slot, a wavefront four of its ranks: lane 4 q + j has tokens 8 q .. of rank j.
+template <typename T> __global__ __launch_bounds__(256) void k8_turn(const K8Turn a) {
+    constexpr bool half = sizeof(T) == 2;
+    constexpr int PARTS = kK8Parts<T>;
+    const int lane = (int)(threadIdx.x & 63u), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int tiles_all = a.rank_pad / 16;
+    const int b = (int)blockIdx.x, at = (int)blockIdx.y, side = (int)blockIdx.z / tiles_all, r = (int)blockIdx.z - side * tiles_all, t0 = b * 128;
+    // u of the tokens, whatever their slots: one latency for all loads.  What no token of the slot's wrote is taken out below
+    const int j4 = lane & 3, q = lane >> 2;
+    const float* p = a.w[side] + (int64_t)(t0 + 8 * q) * a.rank_pad + r * 16 + wave * 4 + j4;
+    float v[8];
+    for (int sp = 0; sp < a.splits[side]; ++sp)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float x = 0.0f;
+            if (t0 + 8 * q + i < a.n) x = p[((int64_t)sp * a.n + i) * a.rank_pad];
+            v[i] = sp ? v[i] + x : x;
+        }
+    const int32_t s0 = t0 + lane < a.n ? a.slot_of[t0 + lane] : -1, s1 = t0 + 64 + lane < a.n ? a.slot_of[t0 + 64 + lane] : -1;
+    const int wanted = a.which[at];
+    const int slot = (uint32_t)wanted < (uint32_t)a.slots ? wanted : -1;
+    const int rank = slot < 0 ? 0 : __builtin_amdgcn_readfirstlane(a.rank[slot]);
+    const uint64_t m0 = rank > 0 ? __builtin_amdgcn_ballot_w64(s0 == slot) : 0, m1 = rank > 0 ? __builtin_amdgcn_ballot_w64(s1 == slot) : 0;
+    if (blockIdx.z == 0 && threadIdx.x == 0) {
+        a.out.masks[(int64_t)at * a.blocks + b] = K8Mask{{m0, m1}};
+        if (b == 0) a.out.slots[at] = K8Slot{rank, slot < 0 ? 0.0f : a.scale[slot], {0, 0}};
+    }
+    if ((m0 | m1) == 0 || r * 16 >= rank) return;
+    const uint32_t byte = (uint32_t)((q < 8 ? m0 : m1) >> (8 * (q & 7))) & 0xffu;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (byte >> i) & 1u ? v[i] : 0.0f;
+    const int64_t part_of = ((int64_t)at * 2 + side) * a.blocks + b;
+    k8_v8<T>* dst = static_cast<k8_v8<T>*>(a.out.w) + ((part_of * tiles_all + r) * 4 + (q >> 2)) * PARTS * 64 + (q & 3) * 16 + wave * 4 + j4;
+    if constexpr (half) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t bits = __builtin_bit_cast(uint32_t, v[i]) & 0x7fffffffu;
+            top = bits < 0x7f800000u && bits > top ? bits : top;
+        }
+#pragma unroll
+        for (int x = 4; x < 64; x *= 2) {
+            const uint32_t o = (uint32_t)__shfl_xor((int)top, x);
+            top = o > top ? o : top;
+        }
+        const int shift = kx_shift(top);
+        const float up = kx_pow2(shift);
+        k8_v8<T> hi, lo;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            _Float16 h, l;
+            kx_parts(v[i] * up, h, l);
+            hi[i] = (T)h, lo[i] = (T)l;
+        }
+        dst[0] = hi, dst[64] = lo;
+        if (q == 0) a.out.down[part_of * a.rank_pad + r * 16 + wave * 4 + j4] = kx_pow2(-shift);
+    } else {
+        k8_v8<T> o;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = (T)v[i];
+        dst[0] = o;
+    }
+}
+
+struct K8Grad {
+    K8Turned in;
+    const void* x;              // [k][n], or int8 [k][x_pitch]
+    const uint8_t* x_scale;     // [block][x_scale_pitch]
+    const void* g;              // [m][n]
     float *da, *db, *work;
     int64_t x_pitch, x_scale_pitch;
-    int32_t m, k, n, slots, rank_pad, max_rank, tiles_k, count, splits, u_splits, v_splits;
+    int32_t m, k, n, blocks, rank_pad, max_rank, tiles_k, count, splits;
 };
 
-// The workgroup's LDS: 128 tokens of RG rank tiles of w, [32 tokens][rank tile][part][64 lanes][8], and a factor for each rank.
-template <typename T, int RG> struct K8GradLds {
-    static constexpr int parts = sizeof(T) == 2 ? 2 : 1;
-    k8_v8<T> w[4][RG][parts][64];
-    float down[RG][16];
-};
-
-// Eight values of z for a lane: row p, tokens t ..  Zeros from `left` on; `byte`: which of the eight tokens are the slot's.
-template <typename T> __device__ __forceinline__ k8_v8<T> k8_z(const T* row, int left, bool row_ok) {
-    T v[8];
-    k8_load<T, 8>(row, row_ok ? left : 0, v);
-    k8_v8<T> z;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] = v[i];
-    return z;
-}
-template <typename T> __device__ __forceinline__ k8_v8<T> k8_z8(const int8_t* row, bool row_ok) {
-    k8_v8<T> z;
-    uint2 q = {0u, 0u};
-    if (row_ok) q = *reinterpret_cast<const uint2*>(row);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) z[i] = (T)(float)(int8_t)((i < 4 ? q.x : q.y) >> (8 * (i & 3)));
-    return z;
-}
-
+// A wavefront takes 16 RW rows, the workgroup's four 64 RW, and of the blocks with a token of the slot's a share; no wavefront waits for
+// another.  z of the next block is on its way while a block is multiplied.  Several shares are joined in order by k8_grad_join.
 template <typename T, int RG, int RW, bool HELD8>
 __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
-    __shared__ K8GradLds<T, RG> lds;
     constexpr bool half = sizeof(T) == 2;
-    constexpr int PARTS = K8GradLds<T, RG>::parts;
+    constexpr int PARTS = kK8Parts<T>;
     const int lane = (int)(threadIdx.x & 63u), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int c = lane & 15, g = lane >> 4;
     const bool of_a = (int)blockIdx.x < a.tiles_k;
     const int rows = of_a ? a.k : a.m;
     const int row0 = ((int)blockIdx.x - (of_a ? 0 : a.tiles_k)) * 64 * RW + wave * 16 * RW;
+    if (row0 >= rows) return;
     const int at = (int)blockIdx.y, split = (int)blockIdx.z;
-    const int wanted = a.which[at];
-    const int slot = (uint32_t)wanted < (uint32_t)a.slots ? wanted : -1;
-    const int rank = slot < 0 ? 0 : __builtin_amdgcn_readfirstlane(a.rank[slot]);
-    const int blocks = (a.n + 127) / 128;
-    const int b0 = (int)((int64_t)blocks * split / a.splits), b1 = (int)((int64_t)blocks * (split + 1) / a.splits);
-    const float* w = of_a ? a.v : a.u;
-    const int w_splits = of_a ? a.v_splits : a.u_splits;
-    const int64_t w_split = (int64_t)a.n * a.rank_pad;
+    const K8Slot slot = a.in.slots[at];
+    const int rank = __builtin_amdgcn_readfirstlane(slot.rank);
     const int tiles_all = a.rank_pad / 16;
+    const K8Mask* masks = a.in.masks + (int64_t)at * a.blocks;
+
+    // 64 blocks at a time, one to a lane
+    auto found = [&](int group) {
+        const int b = group * 64 + lane;
+        bool some = false;
+        if (b < a.blocks) some = (masks[b].half[0] | masks[b].half[1]) != 0;
+        return (uint64_t)__builtin_amdgcn_ballot_w64(some);
+    };
+    const int groups = (a.blocks + 63) / 64;
+    int mine = 0, skip = 0;                                      // this workgroup's share of the blocks found
+    if (rank > 0) {
+        int count = 0;
+        for (int i = 0; i < groups; ++i) count += __builtin_popcountll(found(i));
+        skip = (int)((int64_t)count * split / a.splits);
+        mine = (int)((int64_t)count * (split + 1) / a.splits) - skip;
+    }
 
     for (int rt0 = 0; rt0 < tiles_all; rt0 += RG) {
         const int tiles = min((rank + 15) / 16 - rt0, RG);       // of this slot, here (none: zeros are stored)
+        const int todo = tiles > 0 ? mine : 0;
         k8_f4 acc[RW][RG];
 #pragma unroll
         for (int i = 0; i < RW; ++i)
 #pragma unroll
             for (int r = 0; r < RG; ++r) acc[i][r] = k8_f4(0.0f);
-        for (int b = b0; b < (tiles > 0 ? b1 : b0); ++b) {
+
+        int group = 0;
+        uint64_t left = 0;
+        if (todo > 0) {
+            int over = skip;
+            left = found(0);
+            while (__builtin_popcountll(left) <= over) over -= __builtin_popcountll(left), left = found(++group);
+            for (; over > 0; --over) left &= left - 1;
+        }
+        auto next_block = [&]() {                                // called `todo` times only
+            while (left == 0) left = found(++group);
+            const int b = group * 64 + __builtin_ctzll(left);
+            left &= left - 1;
+            return b;
+        };
+
+        k8_any<T, 8> z[RW][4];                                   // on its way: the next block's
+        uint2 z8[RW][4];
+        uint32_t zs[RW];
+        auto load_z = [&](int b) {
             const int tb = b * 128;
-            const bool in0 = tb + lane < a.n && a.slot_of[tb + lane] == slot, in1 = tb + 64 + lane < a.n && a.slot_of[tb + 64 + lane] == slot;
-            const uint64_t m0 = __builtin_amdgcn_ballot_w64(in0), m1 = __builtin_amdgcn_ballot_w64(in1);
-            if ((m0 | m1) == 0) continue;
-            __syncthreads();                                     // the last block's operands have been read
-            {
-                // a wavefront turns four ranks of each tile: lane 4 q + j has tokens 8 q .. of rank j
-                const int j4 = lane & 3, q = lane >> 2;
-                const uint32_t byte = (uint32_t)((q < 8 ? m0 : m1) >> (8 * (q & 7))) & 0xffu;
-#pragma unroll
-                for (int r = 0; r < RG; ++r)
-                    if (r < tiles) {
-                        const int j = wave * 4 + j4;
-                        const float* p = w + (int64_t)(tb + 8 * q) * a.rank_pad + (rt0 + r) * 16 + j;
-                        float v[8];
-                        uint32_t top = 0;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            v[i] = 0.0f;
-                            if ((byte >> i) & 1u)
-                                for (int sp = 0; sp < w_splits; ++sp) v[i] += p[sp * w_split + (int64_t)i * a.rank_pad];
-                            const uint32_t bits = __builtin_bit_cast(uint32_t, v[i]) & 0x7fffffffu;
-                            if (bits < 0x7f800000u && bits > top) top = bits;
-                        }
-                        const int dst = (q & 3) * 16 + j;
-                        if constexpr (half) {
-#pragma unroll
-                            for (int x = 4; x < 64; x *= 2) {
-                                const uint32_t o = (uint32_t)__shfl_xor((int)top, x);
-                                top = o > top ? o : top;
-                            }
-                            const int shift = kx_shift(top);
-                            const float up = kx_pow2(shift);
-                            k8_v8<T> hi, lo;
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                _Float16 h, l;
-                                kx_parts(v[i] * up, h, l);
-                                hi[i] = (T)h, lo[i] = (T)l;
-                            }
-                            lds.w[q >> 2][r][0][dst] = hi;
-                            lds.w[q >> 2][r][PARTS - 1][dst] = lo;
-                            if (q == 0) lds.down[r][j] = kx_pow2(-shift);
-                        } else {
-                            k8_v8<T> o;
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) o[i] = (T)v[i];
-                            lds.w[q >> 2][r][0][dst] = o;
-                            if (q == 0) lds.down[r][j] = 1.0f;
-                        }
-                    }
-            }
-            __syncthreads();
-            const bool whole = (m0 & m1) == ~0ull;
 #pragma unroll
             for (int i = 0; i < RW; ++i) {
                 const int row = row0 + i * 16 + c;
                 const bool row_ok = row < rows;
-                k8_v8<T> z[4];
+                if (HELD8 && of_a) {
+                    const int8_t* src = static_cast<const int8_t*>(a.x) + (int64_t)row * a.x_pitch + tb + g * 8;
+#pragma unroll
+                    for (int st = 0; st < 4; ++st) {
+                        z8[i][st] = uint2{0u, 0u};
+                        if (row_ok) z8[i][st] = *reinterpret_cast<const uint2*>(src + st * 32);
+                    }
+                    const int r4 = row0 + i * 16 + 4 * g;
+                    zs[i] = 0;
+                    if (r4 < a.x_scale_pitch) zs[i] = *reinterpret_cast<const uint32_t*>(a.x_scale + (int64_t)b * a.x_scale_pitch + r4);
+                } else {
+                    const T* src = static_cast<const T*>(of_a ? a.x : a.g) + (int64_t)row * a.n + tb + g * 8;
+#pragma unroll
+                    for (int st = 0; st < 4; ++st) z[i][st] = k8_load<T, 8>(src + st * 32, row_ok ? a.n - (tb + st * 32 + g * 8) : 0);
+                }
+            }
+        };
+
+        int b = 0;
+        if (todo > 0) b = next_block(), load_z(b);
+        for (int done = 0; done < todo; ++done) {
+            const int64_t part_of = ((int64_t)at * 2 + (of_a ? 0 : 1)) * a.blocks + b;
+            const k8_v8<T>* ops = static_cast<const k8_v8<T>*>(a.in.w) + (part_of * tiles_all + rt0) * 4 * PARTS * 64 + lane;
+            const float* downs = a.in.down + part_of * a.rank_pad + rt0 * 16 + c;
+            k8_v8<T> op[RG > 1 ? 2 : 1][4][PARTS];               // of one rank tile, and of the next
+            float down[2] = {1.0f, 1.0f};
+            auto load_op = [&](int r) {
+#pragma unroll
+                for (int st = 0; st < 4; ++st)
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part) op[r & 1][st][part] = ops[((r * 4 + st) * PARTS + part) * 64];
+                if (half) down[r & 1] = downs[r * 16];
+            };
+            load_op(0);
+            const K8Mask mask = masks[b];
+            const uint64_t m0 = mask.half[0], m1 = mask.half[1];
+            const bool whole = (m0 & m1) == ~0ull;
+            k8_v8<T> cur[RW][4];
+            float scales[RW][4];
+#pragma unroll
+            for (int i = 0; i < RW; ++i) {
 #pragma unroll
                 for (int st = 0; st < 4; ++st) {
-                    const int t = tb + st * 32 + g * 8;
-                    if (HELD8 && of_a) z[st] = k8_z8<T>(static_cast<const int8_t*>(a.x) + (int64_t)row * a.x_pitch + t, row_ok);
-                    else z[st] = k8_z<T>(static_cast<const T*>(of_a ? a.x : a.g) + (int64_t)row * a.n + t, a.n - t, row_ok);
-                    if (!whole) {
+                    if (HELD8 && of_a) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) cur[i][st][e] = (T)(float)(int8_t)((e < 4 ? z8[i][st].x : z8[i][st].y) >> (8 * (e & 3)));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) cur[i][st][e] = z[i][st][e];
+                    }
+                    if (!whole) {                                // tokens of other slots: whatever z holds there, not a number even
                         const uint32_t byte = (uint32_t)((st < 2 ? m0 : m1) >> (32 * (st & 1) + 8 * g)) & 0xffu;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) z[st][e] = (byte >> e) & 1u ? z[st][e] : (T)0.0f;
-                    }
-                }
-                float zs[4] = {1.0f, 1.0f, 1.0f, 1.0f};          // of the rows of this lane's results
-                if (HELD8 && of_a) {
-                    const int r4 = row0 + i * 16 + 4 * g;
-                    uint32_t s4 = 0;
-                    if (r4 < a.x_scale_pitch) s4 = *reinterpret_cast<const uint32_t*>(a.x_scale + (int64_t)b * a.x_scale_pitch + r4);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t s = (s4 >> (8 * e)) & 0xffu;
-                        zs[e] = __builtin_bit_cast(float, s == 255u ? 0x7fc00000u : s << 23);
+                        for (int e = 0; e < 8; ++e) cur[i][st][e] = (byte >> e) & 1u ? cur[i][st][e] : (T)0.0f;
                     }
                 }
 #pragma unroll
-                for (int r = 0; r < RG; ++r)
-                    if (r < tiles) {
-                        k8_f4 sum = k8_f4(0.0f);
-#pragma unroll
-                        for (int st = 0; st < 4; ++st)
-#pragma unroll
-                            for (int part = 0; part < PARTS; ++part) sum = k8_mfma(z[st], lds.w[st][r][part][lane], sum);
-                        const float down = lds.down[r][c];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][r][e] = __builtin_fmaf(sum[e] * down, zs[e], acc[i][r][e]);
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t s = (zs[i] >> (8 * e)) & 0xffu;
+                    scales[i][e] = HELD8 && of_a ? __builtin_bit_cast(float, s == 255u ? 0x7fc00000u : s << 23) : 1.0f;
+                }
             }
+            if (done + 1 < todo) b = next_block(), load_z(b);
+#pragma unroll
+            for (int r = 0; r < RG; ++r)
+                if (r < tiles) {
+                    if (r + 1 < RG && r + 1 < tiles) load_op(r + 1);
+                    k8_f4 sum[RW];
+#pragma unroll
+                    for (int i = 0; i < RW; ++i) sum[i] = k8_f4(0.0f);
+#pragma unroll
+                    for (int st = 0; st < 4; ++st)
+#pragma unroll
+                        for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+                            for (int i = 0; i < RW; ++i) sum[i] = k8_mfma(cur[i][st], op[r & 1][st][part], sum[i]);
+#pragma unroll
+                    for (int i = 0; i < RW; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[i][r][e] = __builtin_fmaf(sum[i][e] * down[r & 1], scales[i][e], acc[i][r][e]);
+                }
         }
         // lane's results: rows 4 g + e, rank c
-        const float factor = slot < 0 ? 0.0f : a.scale[slot];
 #pragma unroll
         for (int i = 0; i < RW; ++i)
 #pragma unroll
             for (int r = 0; r < RG; ++r) {
-                if (rt0 + r >= tiles_all) continue;
+                // k8_grad_join reads the ranks that the slot has, of all shares
+                if (rt0 + r >= tiles_all || (a.splits > 1 && r >= tiles)) continue;
                 const int j = (rt0 + r) * 16 + c, p = row0 + i * 16 + 4 * g;
-                float v[4];
+                k8_any<float, 4> v;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = j < rank ? acc[i][r][e] : 0.0f;
                 if (a.splits > 1) {
@@ -481,7 +597,7 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
                             if (p + e < rows) part[(int64_t)a.rank_pad * a.k + (int64_t)(p + e) * a.rank_pad + j] = v[e];
                 } else if (j < a.max_rank) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = j < rank ? v[e] * factor : 0.0f;
+                    for (int e = 0; e < 4; ++e) v[e] = j < rank ? v[e] * slot.factor : 0.0f;
                     if (of_a) k8_store<float, 4>(a.da + ((int64_t)at * a.max_rank + j) * a.k + p, rows - p, v);
                     else
 #pragma unroll
@@ -494,19 +610,16 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
 
 // Adds the shares up, in order, and takes the slot's factor in.
 struct K8Join {
+    const K8Slot* slots;
     const float* work;
-    const int32_t* which;
-    const int32_t* rank;
-    const float* scale;
     float *da, *db;
-    int32_t m, k, slots, rank_pad, max_rank, count, splits;
+    int32_t m, k, rank_pad, max_rank, count, splits;
 };
 __global__ __launch_bounds__(256) void k8_grad_join(const K8Join a) {
     const int64_t per = ((int64_t)a.k + a.m) * a.max_rank, stride = (int64_t)a.count * ((int64_t)a.k + a.m) * a.rank_pad;
-    const int at = (int)blockIdx.y, wanted = a.which[at];
-    const int slot = (uint32_t)wanted < (uint32_t)a.slots ? wanted : -1;
-    const int rank = slot < 0 ? 0 : a.rank[slot];
-    const float factor = slot < 0 ? 0.0f : a.scale[slot];
+    const int at = (int)blockIdx.y;
+    const int rank = a.slots[at].rank;
+    const float factor = a.slots[at].factor;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < per; i += (int64_t)gridDim.x * 256) {
         const bool of_a = i < (int64_t)a.k * a.max_rank;
         const int64_t o = of_a ? i : i - (int64_t)a.k * a.max_rank;

@@ -144,7 +144,7 @@ template <int NT> struct KxItems {
 
     // u of tile nt, ranks from 16 c on; unwritten memory where a token has no adapter or a lower rank
     __device__ __forceinline__ void load(int nt, int c, float (&v)[1][8]) const {
-        constexpr int B = NT == 1 ? 4 : (NT == 2 ? 2 : 1);      // shares in flight at a time
+        constexpr int B = NT == 1 ? 4 : 2;                      // shares in flight at a time
         for (int s0 = 0; s0 < e.splits; s0 += B) {
             kx_f4 w[B][2];
 #pragma unroll

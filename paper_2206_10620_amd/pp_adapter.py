@@ -100,31 +100,49 @@ def pp_adapter_destroy(bank) -> int:
     return lib().pp_adapter_destroy(bank)
 
 
+_TORCH = None
+
+
+def _torch():
+    """torch, imported when it is first needed (the plain entry points above do without)."""
+    global _TORCH
+    if _TORCH is None:
+        import torch
+        _TORCH = torch
+    return _TORCH
+
+
 def _torch_dtype(dtype: int):
-    import torch
-    return torch.float16 if dtype == PP_F16 else torch.float32
+    t = _TORCH or _torch()
+    return t.float16 if dtype == PP_F16 else t.float32
 
 
 class _Call:
-    """The device and stream of a call: the tensors' device is made current, and what the call allocates belongs to the stream it runs on."""
+    """The device and stream of a call: the tensors' device is made current, and what the call allocates belongs to the stream it
+    runs on.  On the current device and stream, the usual case, nothing has to be changed or put back."""
+
+    __slots__ = ("_device", "_stream", "_index")
 
     def __init__(self, device, stream: Optional[int]):
-        import torch
-        self._device = torch.cuda.device(device)
-        self._stream = None if stream is None else torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device) if stream
-                                                                     else torch.cuda.default_stream(device))
-        self._torch = torch
+        t = _TORCH or _torch()
+        self._index = device.index
+        self._device = None if device.index == t.cuda.current_device() else t.cuda.device(device)
+        self._stream = None
+        if stream is not None:
+            self._stream = t.cuda.stream(t.cuda.ExternalStream(stream, device=device) if stream else t.cuda.default_stream(device))
 
     def __enter__(self) -> int:
-        self._device.__enter__()
+        if self._device is not None:
+            self._device.__enter__()
         if self._stream is not None:
             self._stream.__enter__()
-        return self._torch.cuda.current_stream().cuda_stream
+        return _TORCH.cuda.current_stream(self._index).cuda_stream
 
     def __exit__(self, *exc):
         if self._stream is not None:
             self._stream.__exit__(*exc)
-        self._device.__exit__(*exc)
+        if self._device is not None:
+            self._device.__exit__(*exc)
 
 
 def _check_status(st: int, what: str) -> None:
@@ -146,7 +164,7 @@ class Act8:
 
     def unpack(self, dtype: Optional[int] = None, stream: Optional[int] = None):
         """The values held, as a tensor of dtype (default: that of the tensor that was packed)."""
-        import torch
+        torch = _torch()
         dtype = self.dtype if dtype is None else dtype
         with _Call(self.buffer.device, stream) as s:
             out = torch.empty((self.rows, self.n), dtype=_torch_dtype(dtype), device=self.buffer.device)
@@ -156,7 +174,7 @@ class Act8:
 
 def act8_pack(x, stream: Optional[int] = None) -> Act8:
     """x [rows, n] (fp16 or fp32, on the GPU) in 8 bits."""
-    import torch
+    torch = _torch()
     assert x.is_cuda and x.is_contiguous() and x.dim() == 2 and x.dtype in (torch.float16, torch.float32)
     rows, n = x.shape
     dtype = PP_F16 if x.dtype == torch.float16 else PP_F32
@@ -177,7 +195,7 @@ class AdapterBank:
     """Owns one bank of adapters; the methods take torch tensors only to read their device pointers."""
 
     def __init__(self, m: int, k: int, slots: int, max_rank: int, dtype: int = PP_F16, device=None):
-        import torch
+        torch = _torch()
         self.handle = None
         self.m, self.k, self.slots, self.max_rank, self.dtype = m, k, slots, max_rank, dtype
         self.device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
@@ -186,13 +204,21 @@ class AdapterBank:
         with torch.cuda.device(self.device):
             st, self.handle = pp_adapter_plan(m, k, slots, max_rank, dtype)
         _check_status(st, "pp_adapter_plan")
+        self._sizes = {}                                # n -> bytes of u and v
+
+    def _state_bytes(self, n: int):
+        """Bytes of u and of v for n tokens (0: the call that follows refuses n)."""
+        sizes = self._sizes.get(n)
+        if sizes is None:
+            sizes = self._sizes[n] = (pp_adapter_u_bytes(self.handle, n), pp_adapter_v_bytes(self.handle, n))
+        return sizes
 
     def _slots_of(self, slot_of, n: int):
-        import torch
+        torch = _torch()
         assert slot_of.is_cuda and slot_of.is_contiguous() and slot_of.dtype == torch.int32 and tuple(slot_of.shape) == (n,) and slot_of.device == self.device
 
     def _opaque(self, nbytes: int):
-        import torch
+        torch = _torch()
         return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
 
     def load(self, slot: int, a, b, scale: float, stream: Optional[int] = None) -> None:
@@ -213,13 +239,13 @@ class AdapterBank:
         n = x.shape[1]
         self._slots_of(slot_of, n)
         with _Call(self.device, stream) as s:
-            u = self._opaque(pp_adapter_u_bytes(self.handle, n))
+            u = self._opaque(self._state_bytes(n)[0])
             _check_status(pp_adapter_project(self.handle, x.data_ptr(), slot_of.data_ptr(), u.data_ptr(), n, s), "pp_adapter_project")
         return u
 
     def run(self, plan: BlockPlan, x, slot_of, y=None, keep: bool = False, stream: Optional[int] = None):
         """y = act(W x + bias + c B (A x)); with keep also u, which grad_weights takes."""
-        import torch
+        torch = _torch()
         _matrix(x, self.k, None, self.dtype, self.device)
         n = x.shape[1]
         self._slots_of(slot_of, n)
@@ -227,14 +253,14 @@ class AdapterBank:
             if y is None:
                 y = torch.empty((self.m, n), dtype=x.dtype, device=self.device)
             _matrix(y, self.m, n, self.dtype, self.device)
-            u = self._opaque(pp_adapter_u_bytes(self.handle, n))
+            u = self._opaque(self._state_bytes(n)[0])
             _check_status(pp_adapter_run(self.handle, plan.handle, x.data_ptr(), slot_of.data_ptr(), u.data_ptr(), y.data_ptr(), n, s), "pp_adapter_run")
         return (y, u) if keep else y
 
     def grad_input(self, plan_t: Optional[BlockPlan], dy, slot_of, gate: Optional[Act8] = None, stream: Optional[int] = None) -> InputGradient:
         """dx = W^T g + c A^T (B^T g) through plan_t, the plan of the transposed weights (None: no dx), g = dy where the output held
         in gate is above 0 (None: everywhere)."""
-        import torch
+        torch = _torch()
         _matrix(dy, self.m, None, self.dtype, self.device)
         n = dy.shape[1]
         self._slots_of(slot_of, n)
@@ -242,7 +268,7 @@ class AdapterBank:
         with _Call(self.device, stream) as s:
             g = dy if gate is None else torch.empty_like(dy)
             dx = None if plan_t is None else torch.empty((self.k, n), dtype=dy.dtype, device=self.device)
-            v = self._opaque(pp_adapter_v_bytes(self.handle, n))
+            v = self._opaque(self._state_bytes(n)[1])
             st = pp_adapter_grad_input(self.handle, None if plan_t is None else plan_t.handle, dy.data_ptr(), None if gate is None else gate.buffer.data_ptr(),
                                        None if gate is None else g.data_ptr(), slot_of.data_ptr(), v.data_ptr(), None if dx is None else dx.data_ptr(), n, s)
             _check_status(st, "pp_adapter_grad_input")
@@ -251,7 +277,7 @@ class AdapterBank:
     def grad_weights(self, x: Union["Act8", object], u, g, v, slot_of, which, stream: Optional[int] = None):
         """Gradients of the slots that which (int32 tensor) lists: da [count, max_rank, k], db [count, m, max_rank], fp32.  x: the
         layer's input, as it was or in 8 bits; u of run or project, g and v of grad_input."""
-        import torch
+        torch = _torch()
         _matrix(g, self.m, None, self.dtype, self.device)
         n = g.shape[1]
         self._slots_of(slot_of, n)
@@ -261,7 +287,7 @@ class AdapterBank:
         else:
             _matrix(x, self.k, n, self.dtype, self.device)
         assert which.is_cuda and which.is_contiguous() and which.dtype == torch.int32 and which.dim() == 1 and which.device == self.device
-        assert u.numel() == pp_adapter_u_bytes(self.handle, n) and v.numel() == pp_adapter_v_bytes(self.handle, n)
+        assert (u.numel(), v.numel()) == self._state_bytes(n)
         count = which.shape[0]
         with _Call(self.device, stream) as s:
             da = torch.empty((count, self.max_rank, self.k), dtype=torch.float32, device=self.device)

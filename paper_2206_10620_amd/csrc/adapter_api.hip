@@ -54,7 +54,7 @@ template <typename T, int FT, int RG, bool GATED> void project_as(const K8Projec
     hipLaunchKernelGGL((k8_project<T, FT, RG, GATED>), grid, dim3(64 * kProjectWaves), 0, stream, a);
 }
 template <typename T, int FT, bool GATED> void project_rg(const K8Project& a, dim3 grid, hipStream_t stream) {
-    constexpr int most = sizeof(T) == 4 && FT == 4 ? 2 : 4;      // rank tiles in registers at a time: four would spill there
+    constexpr int most = (sizeof(T) == 4 && FT == 4) || FT == 8 ? 2 : 4;      // rank tiles in registers at a time: four would spill there
     if (a.rank_pad <= 16) project_as<T, FT, 1, GATED>(a, grid, stream);
     else if (a.rank_pad <= 32) project_as<T, FT, 2, GATED>(a, grid, stream);
     else project_as<T, FT, most, GATED>(a, grid, stream);
@@ -62,7 +62,8 @@ template <typename T, int FT, bool GATED> void project_rg(const K8Project& a, di
 template <typename T, bool GATED> void project_ft(int ft, const K8Project& a, dim3 grid, hipStream_t stream) {
     if (ft == 1) project_rg<T, 1, GATED>(a, grid, stream);
     else if (ft == 2) project_rg<T, 2, GATED>(a, grid, stream);
-    else project_rg<T, 4, GATED>(a, grid, stream);
+    else if (ft == 4) project_rg<T, 4, GATED>(a, grid, stream);
+    else if constexpr (GATED && sizeof(T) == 2) project_rg<T, 8, GATED>(a, grid, stream);
 }
 
 // where the sums of what a projection left start
@@ -80,13 +81,14 @@ void launch_project(const pp_adapter_bank_t* b, bool of_a, const void* x, const 
     a.slot_elems = (of_a ? b->a_project_slot : b->b_project_slot) / elem(b);
     a.gate_pitch = act8_pitch(n);
     a.n = n, a.steps = (a.rows + 31) / 32, a.slots = b->slots, a.rank_pad = b->rank_pad, a.splits = sh.splits;
-    const dim3 grid((unsigned)(sh.tiles * sh.splits), (unsigned)project_subsets(sh, b->slots));
+    const int ft = project_tokens(sh, gate != nullptr, b->dtype == PP_F16, b->rank_pad), tiles = (n + 16 * ft - 1) / (16 * ft);
+    const dim3 grid((unsigned)(tiles * sh.splits), (unsigned)project_subsets(tiles, sh.splits, ft, b->slots));
     if (b->dtype == PP_F16) {
-        if (gate) project_ft<_Float16, true>(sh.ft, a, grid, stream);
-        else project_ft<_Float16, false>(sh.ft, a, grid, stream);
+        if (gate) project_ft<_Float16, true>(ft, a, grid, stream);
+        else project_ft<_Float16, false>(ft, a, grid, stream);
     } else {
-        if (gate) project_ft<float, true>(sh.ft, a, grid, stream);
-        else project_ft<float, false>(sh.ft, a, grid, stream);
+        if (gate) project_ft<float, true>(ft, a, grid, stream);
+        else project_ft<float, false>(ft, a, grid, stream);
     }
 }
 
@@ -95,7 +97,7 @@ pp_status_t launch_product(const pp_adapter_bank_t* b, bool of_b, const pp_block
                            hipStream_t stream) {
     const int rows_in = of_b ? b->k : b->m;
     const int splits = project_shape(rows_in, n, !of_b).splits;
-    const int64_t split_elems = (int64_t)n * b->rank_pad;
+    const int64_t split_elems = kx_share(n, b->rank_pad);
     if (b->dtype == PP_F16) {
         K4Expand e{};
         e.tokens = static_cast<const KxToken*>(u), e.u = sums_of(u, n);
@@ -326,8 +328,9 @@ pp_status_t pp_adapter_grad_weights(const pp_adapter_bank_t* bank, const void* x
         K8Join j{};
         j.slots = turned.slots, j.work = a.work, j.da = da_dev, j.db = db_dev;
         j.m = bank->m, j.k = bank->k, j.rank_pad = bank->rank_pad, j.max_rank = bank->max_rank, j.count = count, j.splits = sh.splits;
-        const int64_t wgs = (((int64_t)bank->k + bank->m) * bank->max_rank + 255) / 256;
-        hipLaunchKernelGGL(k8_grad_join, dim3((unsigned)(wgs < 65536 ? wgs : 65536), (unsigned)count), dim3(256), 0, stream, j);
+        j.wgs_a = ((int64_t)bank->k * bank->max_rank + 255) / 256;
+        const int64_t wgs = j.wgs_a + ((int64_t)bank->m * bank->max_rank + 255) / 256;
+        hipLaunchKernelGGL(k8_grad_join, dim3((unsigned)wgs, (unsigned)count), dim3(256), 0, stream, j);
     }
     return launched();
 }

@@ -24,9 +24,17 @@ struct KxToken {
     int32_t unused;
 };
 
+// u of 32 tokens and 16 ranks stands as the matrix instruction's lanes take it, in two planes of 16 bytes a lane: every load and store of
+// it is a run of 512 bytes or more.  Laid out [token][rank] a lane's load met a line of its own: 4096 x 4096 on 4096 tokens of
+// ranks up to 32 took 2 us more.  The plain offset of (token, rank), of a multiple of four ranks:
+__host__ __device__ __forceinline__ int64_t kx_at(int64_t token, int rank, int rank_pad) {
+    return ((token >> 5) * (rank_pad >> 4) + (rank >> 4)) * 512 + ((rank >> 2) & 1) * 256 + (((rank >> 3) & 1) * 32 + (int)(token & 31)) * 4;
+}
+__host__ __device__ __forceinline__ int64_t kx_share(int64_t n, int rank_pad) { return (n + 31) / 32 * 32 * rank_pad; }      // elements of a share
+
 struct K4Expand {
     const KxToken* tokens;      // [n]
-    const float* u;             // [splits][n][rank_pad]
+    const float* u;             // [splits][kx_share], kx_at
     const void* operands;       // [slot][64-row tile][rank_pad / 16][2][64 lanes][8] binary16
     int64_t slot_bytes, split_elems;
     int32_t splits, rank_pad;
@@ -135,66 +143,75 @@ __device__ __forceinline__ uint32_t kx_leaders(int slot) {
     return valid & ~later;
 }
 
-// The adapters' part of a wavefront's product, 32 columns and 16 ranks at a time.
-template <int NT> struct KxItems {
+// The adapters' part of a wavefront's product, 16 ranks at a time: u of all its tokens, whatever their slots, is loaded at once, without
+// a branch between the loads that would make each wait for the last, then tile by tile of 32 columns the slots are gone through.
+// Of `parts` wavefronts with the same columns this one takes every by_chunk-th 16 ranks and every by_slot-th slot from my_slot on.
+template <int NT, int D> struct KxItems {
+    static constexpr int kShares = NT == 1 ? 4 : 2;             // of u at once; there are seldom more
+    static constexpr int kAtOnce = NT == 4 ? 2 : NT;            // tiles; four would not fit the registers beside their accumulators
+    struct Operand {
+        kx_h8 v[2];
+        int slot;               // whose it is, -1 for nobody's
+    };
     const K4Expand& e;
-    int t0, n;
+    int my_slot, by_slot;
     const float* u0;
     const unsigned char* ops0;
 
-    // u of tile nt, ranks from 16 c on; unwritten memory where a token has no adapter or a lower rank
-    __device__ __forceinline__ void load(int nt, int c, float (&v)[1][8]) const {
-        constexpr int B = NT == 1 ? 4 : 2;                      // shares in flight at a time
-        for (int s0 = 0; s0 < e.splits; s0 += B) {
-            kx_f4 w[B][2];
+    // ranks from 16 c on; unwritten memory where a token has no adapter or a lower rank.  tile: 0 .. NT - 1, one that there is
+    __device__ __forceinline__ const float* at(int share, int tile, int c) const {
+        return u0 + share * e.split_elems + (tile * (e.rank_pad / 16) + c) * 512;
+    }
+    __device__ __forceinline__ void load(int tile, int c, kx_f4 (&w)[kShares][2]) const {
 #pragma unroll
-            for (int b = 0; b < B; ++b) {
-                w[b][0] = kx_f4(0.0f), w[b][1] = kx_f4(0.0f);
-                if (s0 + b < e.splits && c * 16 < e.rank_pad && t0 + nt * 32 < n) {
-                    const kx_f4* p = reinterpret_cast<const kx_f4*>(u0 + (s0 + b) * e.split_elems + (int64_t)(nt * 32) * e.rank_pad + c * 16);
-                    w[b][0] = p[0], w[b][1] = p[1];
-                }
-            }
+        for (int b = 0; b < kShares; ++b) {
+            const kx_f4* p = reinterpret_cast<const kx_f4*>(at(b < e.splits ? b : 0, tile, c));
+            w[b][0] = p[0], w[b][1] = p[64];
+        }
+    }
+    __device__ __forceinline__ void sum(int tile, int c, const kx_f4 (&w)[kShares][2], float (&v)[1][8]) const {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                float x = w[0][q >> 2][q & 3];
+        for (int q = 0; q < 8; ++q) {
+            v[0][q] = w[0][q >> 2][q & 3];
 #pragma unroll
-                for (int b = 1; b < B; ++b) x += w[b][q >> 2][q & 3];
-                v[0][q] = s0 ? v[0][q] + x : x;
-            }
+            for (int b = 1; b < kShares; ++b) v[0][q] += b < e.splits ? w[b][q >> 2][q & 3] : 0.0f;
+        }
+        for (int s = kShares; s < e.splits; ++s) {
+            const kx_f4* p = reinterpret_cast<const kx_f4*>(at(s, tile, c));
+            const kx_f4 x = p[0], y = p[64];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[0][q] += x[q], v[0][4 + q] += y[q];
         }
     }
 
-    struct Operand {
-        kx_h8 v[2];
-        int slot;               // whose it is
-    };
+    __device__ __forceinline__ void fetch(int s, int c, Operand& to) const {
+        if (to.slot == s) return;
+        const unsigned char* ops = ops0 + s * e.slot_bytes + c * 2048;
+        to.v[0] = *reinterpret_cast<const kx_h8*>(ops), to.v[1] = *reinterpret_cast<const kx_h8*>(ops + 1024);
+        to.slot = s;
+    }
 
-    // Every lane splits its own token's u, whatever its slot, so that one latency serves all tokens; then the slots are gone
-    // through, D of them with their B on the way at once.  b may hold a slot's from the tile before, of the same ranks.  Of the slots
-    // (those of the leaders) every `parts`-th is this wavefront's.
-    template <int NTI, int D>
-    __device__ __forceinline__ void multiply(int c, const KxToken& tok, uint32_t leaders, int part, int parts, float (&v)[1][8], Operand (&b)[D],
-                                             kx_f16 (&acc)[2][NT]) const {
+    // The slots (those of the leaders) with ranks from 16 c on that are this wavefront's, as a mask of their first lanes
+    __device__ __forceinline__ uint32_t slots_of(const KxToken& tok, uint32_t leaders, int c) const {
         uint32_t left = leaders & (uint32_t)__builtin_amdgcn_ballot_w64(tok.rank > c * 16);
-        if (left == 0) return;
-        for (int i = 0; i < part; ++i) left &= left - 1;
-        if (left == 0) return;
+        for (int i = 0; i < my_slot; ++i) left &= left - 1;
+        return left;
+    }
+
+    // Tile NTI: D slots have their B on the way at once.  b may hold one's, of the tile before.
+    template <int NTI>
+    __device__ __forceinline__ void multiply(int c, const KxToken& tok, uint32_t left, float (&v)[1][8], Operand (&b)[D], kx_f16 (&acc)[2][NT]) const {
         bool have[D];
-        auto fetch = [&](Operand& to, bool& got) {
-            got = left != 0;
-            if (got) {
+        auto next = [&](int d) {
+            have[d] = left != 0;
+            if (have[d]) {
                 const int s = __builtin_amdgcn_readlane(tok.slot, __builtin_ctz(left));
-                for (int i = 0; i < parts; ++i) left &= left - 1;
-                if (to.slot != s) {
-                    const unsigned char* ops = ops0 + s * e.slot_bytes + c * 2048;
-                    to.v[0] = *reinterpret_cast<const kx_h8*>(ops), to.v[1] = *reinterpret_cast<const kx_h8*>(ops + 1024);
-                    to.slot = s;
-                }
+                for (int i = 0; i < by_slot; ++i) left &= left - 1;
+                fetch(s, c, b[d]);
             }
         };
 #pragma unroll
-        for (int d = 0; d < D; ++d) fetch(b[d], have[d]);
+        for (int d = 0; d < D; ++d) next(d);
         kx_h8 hi[1], lo[1];
         float down;
 #pragma unroll
@@ -219,61 +236,60 @@ template <int NT> struct KxItems {
                 }
             }
 #pragma unroll
-            for (int d = 0; d < D; ++d) fetch(b[d], have[d]);
+            for (int d = 0; d < D; ++d) next(d);
         }
+    }
+    template <int NTI>
+    __device__ __forceinline__ void tiles(int c, const KxToken (&tok)[NT], const uint32_t (&leaders)[NT], const int (&tile)[NT], kx_f4 (&w)[kAtOnce][kShares][2],
+                                          Operand (&b)[D], kx_f16 (&acc)[2][NT]) const {
+        if constexpr (NTI % kAtOnce == 0) {
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) load(tile[NTI + i], c, w[i]);
+        }
+        const uint32_t left = slots_of(tok[NTI], leaders[NTI], c);
+        if (left) {
+            float v[1][8];
+            sum(tile[NTI], c, w[NTI % kAtOnce], v);
+            multiply<NTI>(c, tok[NTI], left, v, b, acc);
+        }
+        if constexpr (NTI + 1 < NT) tiles<NTI + 1>(c, tok, leaders, tile, w, b, acc);
     }
 };
 
 // Adds to acc (two 32-row tiles of row tile rt by NT tiles of 32 columns from col0) the adapters' part, or, of `parts` wavefronts
-// with the same columns, the part of wavefront `part`: they deal the ranks' chunks out among them first, then the slots.
+// with the same columns, the part of wavefront `part`: they deal the ranks out among them first, 16 at a time, then the slots.
 template <int NT>
 __device__ __forceinline__ void k4_expand(const K4Expand& e, kx_f16 (&acc)[2][NT], int col0, int n, int rt, int lane, int part, int parts) {
     constexpr int D = NT == 1 ? 8 : (NT == 2 ? 4 : 1);
-    KxItems<NT> items = {e, col0 + (lane & 31), n};
-    items.u0 = e.u + (int64_t)items.t0 * e.rank_pad + 8 * (lane >> 5);
-    items.ops0 = static_cast<const unsigned char*>(e.operands) + (int64_t)rt * (e.rank_pad / 16) * 2048 + lane * 16;
+    if (col0 >= n) return;
     int by_chunk = 1;
     while (by_chunk < parts && 2 * by_chunk * 16 <= e.rank_pad) by_chunk *= 2;
-    const int by_slot = parts / by_chunk, c0 = part % by_chunk, my_slot = part / by_chunk;
-    float v[1][8], v2[1][8];
-    items.load(0, c0, v);
+    const int c0 = part % by_chunk;
+    const KxItems<NT, D> items = {e, part / by_chunk, parts / by_chunk, e.u + kx_at(col0, 0, e.rank_pad) + lane * 4,
+                                  static_cast<const unsigned char*>(e.operands) + (int64_t)rt * (e.rank_pad / 16) * 2048 + lane * 16};
     KxToken tok[NT];
-    uint32_t leaders[NT];
-    int top = 0;
+    int tile[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-        tok[nt] = KxToken{-1, 0, 0.0f, 0};
-        if (items.t0 + nt * 32 < n) tok[nt] = e.tokens[items.t0 + nt * 32];
-        top = tok[nt].rank > top ? tok[nt].rank : top;
+        const int t = col0 + nt * 32 + (lane & 31);
+        tok[nt] = e.tokens[t < n ? t : n - 1];
+        tile[nt] = col0 + nt * 32 < n ? nt : 0;
     }
-    if (__builtin_amdgcn_ballot_w64(top > c0 * 16) == 0) return;
+    kx_f4 w[KxItems<NT, D>::kAtOnce][KxItems<NT, D>::kShares][2];
+    int top = 0;
+    uint32_t leaders[NT];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) leaders[nt] = kx_leaders(tok[nt].slot);
+    for (int nt = 0; nt < NT; ++nt) {
+        if (col0 + nt * 32 + (lane & 31) >= n) tok[nt].slot = -1, tok[nt].rank = 0;
+        top = tok[nt].rank > top ? tok[nt].rank : top;
+        leaders[nt] = kx_leaders(tok[nt].slot);
+    }
 #pragma unroll 1
     for (int c = c0; __builtin_amdgcn_ballot_w64(top > c * 16); c += by_chunk) {
-        typename KxItems<NT>::Operand b[D];
+        typename KxItems<NT, D>::Operand b[D];
 #pragma unroll
         for (int d = 0; d < D; ++d) b[d].slot = -1;
-        if constexpr (NT == 4) {
-            items.load(1, c, v2);
-            items.template multiply<0, D>(c, tok[0], leaders[0], my_slot, by_slot, v, b, acc);
-            items.load(2, c, v);
-            items.template multiply<1, D>(c, tok[1], leaders[1], my_slot, by_slot, v2, b, acc);
-            items.load(3, c, v2);
-            items.template multiply<2, D>(c, tok[2], leaders[2], my_slot, by_slot, v, b, acc);
-            items.load(0, c + by_chunk, v);
-            items.template multiply<3, D>(c, tok[3], leaders[3], my_slot, by_slot, v2, b, acc);
-        } else if constexpr (NT == 2) {
-            items.load(1, c, v2);
-            items.template multiply<0, D>(c, tok[0], leaders[0], my_slot, by_slot, v, b, acc);
-            items.load(0, c + by_chunk, v);
-            items.template multiply<1, D>(c, tok[1], leaders[1], my_slot, by_slot, v2, b, acc);
-        } else {
-            items.load(0, c + by_chunk, v2);
-            items.template multiply<0, D>(c, tok[0], leaders[0], my_slot, by_slot, v, b, acc);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) v[0][q] = v2[0][q];
-        }
+        items.template tiles<0>(c, tok, leaders, tile, w, b, acc);
     }
 }
 

@@ -112,7 +112,7 @@ struct K8Project {
     const int8_t* gate;         // [rows][gate_pitch]
     void* g;                    // [rows][n]
     KxToken* tokens;            // [n]
-    float* u;                   // [splits][n][rank_pad]
+    float* u;                   // [splits][kx_share], kx_at
     const int32_t* slot_of;
     const int32_t* rank;
     const float* scale;
@@ -132,7 +132,7 @@ __global__ __launch_bounds__(64 * kProjectWaves) void k8_project(const K8Project
     const int w0 = s0 + (int)((int64_t)(s1 - s0) * wave / W), w1 = s0 + (int)((int64_t)(s1 - s0) * (wave + 1) / W);
     const int left = a.n - mine0;
     const T* x = static_cast<const T*>(a.x);
-    float* u = a.u + (int64_t)split * a.n * a.rank_pad;
+    float* u = a.u + split * kx_share(a.n, a.rank_pad);
 
     typedef k8_any<T, FT> Piece;
     auto load = [&](int st, Piece (&v)[8], bool write_g) {
@@ -202,7 +202,7 @@ __global__ __launch_bounds__(64 * kProjectWaves) void k8_project(const K8Project
                     for (int w = 1; w < W; ++w) v += red[w * FT * 64 + i];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) v[e] = j + e < rank ? v[e] : 0.0f;
-                    if (t < a.n && a.slot_of[t] == slot) *reinterpret_cast<k8_f4*>(u + (int64_t)t * a.rank_pad + j) = v;
+                    if (t < a.n && a.slot_of[t] == slot) *reinterpret_cast<k8_f4*>(u + kx_at(t, j, a.rank_pad)) = v;
                 }
             }
         }
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(64 * kProjectWaves) void k8_project(const K8Project
 struct K8Expand {
     float* y;                   // [m][n]
     const KxToken* tokens;      // [n]
-    const float* u;             // [splits][n][rank_pad]
+    const float* u;             // [splits][kx_share], kx_at
     const float* operands;      // [slot][m][rank_pad]
     int64_t slot_elems, split_elems;
     int32_t m, n, splits, rank_pad, relu;
@@ -269,7 +269,6 @@ __global__ __launch_bounds__(256) void k8_expand_f32(const K8Expand a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = k8_load<float, 4>(a.y + (int64_t)(row0 + 4 * g + i) * a.n + t0, row0 + 4 * g + i < a.m ? left : 0);
     if (!a.relu && __builtin_amdgcn_ballot_w64(any) == 0) return;
-    const float* up = a.u + (int64_t)t0 * a.rank_pad + 4 * g;
     const float* ops0 = a.operands + (int64_t)(row0 + c) * a.rank_pad + 4 * g;
     for (int r0 = 0; r0 < a.rank_pad; r0 += 16) {
         // every lane its own tokens' u, whatever their slots; then slot by slot
@@ -281,7 +280,7 @@ __global__ __launch_bounds__(256) void k8_expand_f32(const K8Expand a) {
 #pragma unroll
                 for (int f = 0; f < 4; ++f) {
                     v[b][f] = k8_f4(0.0f);
-                    if (s0 + b < a.splits && f < left) v[b][f] = *reinterpret_cast<const k8_f4*>(up + (s0 + b) * a.split_elems + (int64_t)f * a.rank_pad + r0);
+                    if (s0 + b < a.splits && f < left) v[b][f] = *reinterpret_cast<const k8_f4*>(a.u + (s0 + b) * a.split_elems + kx_at(t0 + f, r0 + 4 * g, a.rank_pad));
                 }
 #pragma unroll
             for (int f = 0; f < 4; ++f) {
@@ -346,7 +345,7 @@ template <typename T> constexpr int kK8Parts = sizeof(T) == 2 ? 2 : 1;
 struct K8Turn {
     K8Turned out;
     const KxToken* tokens;
-    const float* w[2];          // v, u: [splits][n][rank_pad]
+    const float* w[2];          // v, u: [splits][kx_share], kx_at
     const int32_t* slot_of;
     const int32_t* which;
     const int32_t* rank;
@@ -363,13 +362,14 @@ template <typename T> __global__ __launch_bounds__(256) void k8_turn(const K8Tur
     const int b = (int)blockIdx.x, at = (int)blockIdx.y, side = (int)blockIdx.z / tiles_all, r = (int)blockIdx.z - side * tiles_all, t0 = b * 128;
     // u of the tokens, whatever their slots: one latency for all loads.  What no token of the slot's wrote is taken out below
     const int j4 = lane & 3, q = lane >> 2;
-    const float* p = a.w[side] + (int64_t)(t0 + 8 * q) * a.rank_pad + r * 16 + wave * 4 + j4;
+    const float* p = a.w[side] + kx_at(t0 + 8 * q, r * 16 + wave * 4, a.rank_pad) + j4;      // tokens of a group of eight follow each other
+    const int64_t share = kx_share(a.n, a.rank_pad);
     float v[8];
     for (int sp = 0; sp < a.splits[side]; ++sp)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             float x = 0.0f;
-            if (t0 + 8 * q + i < a.n) x = p[((int64_t)sp * a.n + i) * a.rank_pad];
+            if (t0 + 8 * q + i < a.n) x = p[sp * share + i * 4];
             v[i] = sp ? v[i] + x : x;
         }
     const int32_t s0 = t0 + lane < a.n ? a.slot_of[t0 + lane] : -1, s1 = t0 + 64 + lane < a.n ? a.slot_of[t0 + 64 + lane] : -1;
@@ -613,27 +613,36 @@ struct K8Join {
     const K8Slot* slots;
     const float* work;
     float *da, *db;
+    int64_t wgs_a;              // workgroups of 256 values of A's gradient; B's follow
     int32_t m, k, rank_pad, max_rank, count, splits;
 };
 __global__ __launch_bounds__(256) void k8_grad_join(const K8Join a) {
-    const int64_t per = ((int64_t)a.k + a.m) * a.max_rank, stride = (int64_t)a.count * ((int64_t)a.k + a.m) * a.rank_pad;
     const int at = (int)blockIdx.y;
-    const int rank = a.slots[at].rank;
-    const float factor = a.slots[at].factor;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < per; i += (int64_t)gridDim.x * 256) {
-        const bool of_a = i < (int64_t)a.k * a.max_rank;
-        const int64_t o = of_a ? i : i - (int64_t)a.k * a.max_rank;
-        const int j = of_a ? (int)(o / a.k) : (int)(o % a.max_rank);
-        float v = 0.0f;
-        if (j < rank) {
-            const int64_t src = of_a ? o : (int64_t)a.rank_pad * a.k + o / a.max_rank * a.rank_pad + j;
-            const float* p = a.work + (int64_t)at * ((int64_t)a.k + a.m) * a.rank_pad + src;
-            for (int sp = 0; sp < a.splits; ++sp) v += p[sp * stride];
-            v *= factor;
-        }
-        if (of_a) a.da[(int64_t)at * a.k * a.max_rank + o] = v;
-        else a.db[(int64_t)at * a.m * a.max_rank + o] = v;
+    const bool of_a = (int64_t)blockIdx.x < a.wgs_a;
+    const int64_t first = ((int64_t)blockIdx.x - (of_a ? 0 : a.wgs_a)) * 256, o = first + threadIdx.x;
+    if (o >= (int64_t)(of_a ? a.k : a.m) * a.max_rank) return;
+    const int64_t per = ((int64_t)a.k + a.m) * a.rank_pad, stride = a.count * per;
+    // in a share: A's [rank_pad][k], B's [m][rank_pad]
+    int64_t src = o;
+    int j = 0;
+    if (!of_a) {
+        const int64_t row = first / a.max_rank;                  // the workgroup's first row, once for all lanes
+        const uint32_t off = (uint32_t)(first - row * a.max_rank) + threadIdx.x;
+        j = (int)(off % (uint32_t)a.max_rank);
+        src = (int64_t)a.rank_pad * a.k + (row + off / (uint32_t)a.max_rank) * a.rank_pad + j;
     }
+    const float* p = a.work + at * per + src;
+    const K8Slot slot = a.slots[at];
+    const bool some = of_a ? o < (int64_t)slot.rank * a.k : j < slot.rank;
+    float v[8], sum = 0.0f;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+        v[s] = 0.0f;
+        if (some && s < a.splits) v[s] = p[s * stride];
+    }
+#pragma unroll
+    for (int s = 0; s < 8; ++s) sum += v[s];
+    (of_a ? a.da + (int64_t)at * a.k * a.max_rank : a.db + (int64_t)at * a.m * a.max_rank)[o] = some ? sum * slot.factor : 0.0f;
 }
 
 }  // namespace ppc

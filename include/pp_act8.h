@@ -38,8 +38,8 @@ int64_t pp_act8_bytes(int32_t rows, int32_t n);
  * (PP_ERR_ALIGN otherwise).  PP_ERR_SHAPE: a size < 1, or rows * n beyond 2^31 - 1.  PP_ERR_UNSUPPORTED: an unknown dtype. */
 pp_status_t pp_act8_pack(const void *x_dev, int32_t rows, int32_t n, int32_t dtype, void *held_dev, void *hip_stream);
 
-/* Enqueue the values held, as x_dev [rows][n] of dtype.  PP_F16: a value above 65504, which only an x above 65024 leads to,
- * becomes 65504 of its sign.  Same refusals. */
+/* Enqueue the values held, as x_dev [rows][n] of dtype.  A value beyond dtype's largest number, which in the dtype that was packed only
+ * an x above 127 / 128 of it leads to, becomes that number, of its sign.  Same refusals. */
 pp_status_t pp_act8_unpack(const void *held_dev, int32_t rows, int32_t n, int32_t dtype, void *x_dev, void *hip_stream);
 
 #ifdef __cplusplus

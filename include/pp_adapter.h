@@ -21,8 +21,9 @@
  * Storage is the bank's dtype for x, y, dy, g, dx, A and B; sums, u, v and the gradients of A and B are binary32.  In a
  * PP_F16 bank u and v enter products as two binary16 parts with a power of two taken out, which leaves them 22 bits.
  *
- * Pointers named *_dev are device pointers to the device the bank was made on, which has to be current (PP_ERR_DEVICE
- * otherwise).  Matrices are row-major without gaps and 16-byte aligned.  Runs only read the bank and the plan: any number may be in flight at
+ * Pointers named *_dev are device pointers to the device the bank was made on, which has to be current, and the plan's
+ * (PP_ERR_DEVICE otherwise).  Matrices are row-major without gaps and 16-byte aligned, lists of
+ * slots 4-byte aligned.  Runs only read the bank and the plan: any number may be in flight at
  * once, each with buffers of its own.  A load of a slot is ordered against its uses by the caller (one stream does).
  * Status codes, dtypes and flags are those of pp_conv.h.  Validation comes before any device call.  No call throws; none but plan and destroy
  * synchronises or allocates, so all others can be captured into a graph.
@@ -43,7 +44,7 @@ extern "C" {
 typedef struct pp_adapter_bank pp_adapter_bank_t; /* opaque; owned by the library */
 
 typedef struct {
-    int32_t m, k;        /* rows (outputs) and columns (inputs) of the layer, >= 1, m * k at most 2^31 - 1 */
+    int32_t m, k;        /* rows (outputs) and columns (inputs) of the layer, 1 .. 4194304, m * k at most 2^31 - 1 */
     int32_t slots;       /* 1 .. 65536 */
     int32_t max_rank;    /* the largest rank a slot can take, 1 .. 128 */
     int32_t dtype;       /* pp_dtype_t */
@@ -56,7 +57,8 @@ typedef struct {
 pp_status_t pp_adapter_plan(const pp_adapter_desc_t *desc, pp_adapter_bank_t **out_bank);
 
 /* Enqueue the loading of a slot: a_dev [rank][k], b_dev [m][rank] are copied into the orders that the kernels read, for
- * both directions.  rank 0 empties the slot (a_dev and b_dev are not read).  PP_ERR_SHAPE: a slot or rank out of range. */
+ * both directions.  rank 0 empties the slot (a_dev and b_dev are not read).  PP_ERR_SHAPE: a slot or rank out of
+ * range.  PP_ERR_UNSUPPORTED: a scale that is not finite. */
 pp_status_t pp_adapter_load(pp_adapter_bank_t *bank, int32_t slot, int32_t rank, float scale, const void *a_dev, const void *b_dev, void *hip_stream);
 
 /* Sizes of what a run leaves for the backward pass, for n tokens: u (of A x) and v (of B^T g), opaque, 16-byte aligned.

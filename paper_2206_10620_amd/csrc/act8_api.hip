@@ -57,8 +57,8 @@ template <typename T> __global__ __launch_bounds__(256) void act8_pack(const Act
         k8_any<T, 8> v[kAct8Ahead];
 #pragma unroll
         for (int u = 0; u < kAct8Ahead; ++u) {
-            const int t = (b0 + u) * kAct8Block + part * 8;
-            v[u] = k8_load<T, 8>(src + t, a.n - t);
+            const int64_t t = (int64_t)(b0 + u) * kAct8Block + part * 8;         // behind the last block it may pass 31 bits
+            v[u] = k8_load<T, 8>(src + t, t < a.n ? a.n - (int)t : 0);
         }
 #pragma unroll
         for (int u = 0; u < kAct8Ahead; ++u) {
@@ -89,7 +89,7 @@ template <typename T> __global__ __launch_bounds__(256) void act8_pack(const Act
 #pragma unroll
             for (int i = 0; i < 2; ++i)
                 word[i] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[4 * i + 3], q[4 * i + 2], 0x0c0c0400u), __builtin_amdgcn_perm(q[4 * i + 1], q[4 * i], 0x0c0c0400u), 0x05040100u);
-            *reinterpret_cast<uint2*>(a.q + (int64_t)row * a.pitch + b * kAct8Block + part * 8) = uint2{word[0], word[1]};
+            *reinterpret_cast<uint2*>(a.q + (int64_t)row * a.pitch + (int64_t)b * kAct8Block + part * 8) = uint2{word[0], word[1]};
             if (part == 0) a.scale[(int64_t)b * a.scale_pitch + row] = (uint8_t)(bad ? 255 : e + 127);
         }
     }
@@ -104,22 +104,23 @@ template <typename T> __global__ __launch_bounds__(256) void act8_unpack(const A
 #pragma unroll
         for (int u = 0; u < kAct8Ahead; ++u) {
             const int b = b0 + u < a.blocks ? b0 + u : a.blocks - 1;
-            q[u] = *reinterpret_cast<const uint2*>(a.q + (int64_t)row * a.pitch + b * kAct8Block + part * 8);
+            q[u] = *reinterpret_cast<const uint2*>(a.q + (int64_t)row * a.pitch + (int64_t)b * kAct8Block + part * 8);
             s[u] = a.scale[(int64_t)b * a.scale_pitch + row];
         }
         T* dst = const_cast<T*>(static_cast<const T*>(a.x)) + (int64_t)row * a.n;
 #pragma unroll
         for (int u = 0; u < kAct8Ahead; ++u) {
-            const int t = (b0 + u) * kAct8Block + part * 8;
+            const int64_t t = (int64_t)(b0 + u) * kAct8Block + part * 8;
             const float factor = __builtin_bit_cast(float, s[u] == 255u ? 0x7fc00000u : s[u] << 23);
             k8_any<T, 8> v;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 float f = (float)(int8_t)((i < 4 ? q[u].x : q[u].y) >> (8 * (i & 3))) * factor;
-                if (sizeof(T) == 2) f = f > 65504.0f ? 65504.0f : (f < -65504.0f ? -65504.0f : f);
+                constexpr float most = sizeof(T) == 2 ? 65504.0f : 3.4028235e38f;
+                f = f > most ? most : (f < -most ? -most : f);   // (a NaN stays one)
                 v[i] = (T)f;
             }
-            k8_store<T, 8>(dst + t, a.n - t, v);
+            k8_store<T, 8>(dst + t, t < a.n ? a.n - (int)t : 0, v);
         }
     }
 }

@@ -1,6 +1,7 @@
 // C ABI of the low-rank adapters (include/pp_adapter.h): the bank, checks, launches.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <new>
 
 #include "adapter_rules.hpp"
@@ -31,6 +32,7 @@ struct Range {
 };
 bool overlap(const Range& a, const Range& b) { return a.from < b.to && b.from < a.to; }
 bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+bool misaligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
 int64_t elem(const pp_adapter_bank_t* b) { return b->dtype == PP_F16 ? 2 : 4; }
 
 bool tokens_ok(const pp_adapter_bank_t* b, int32_t n) {
@@ -45,7 +47,9 @@ pp_status_t plan_fits(const pp_adapter_bank_t* b, const pp_block_gemm_plan_t* pl
     const BlockPlanFacts f = block_plan_facts(plan);
     if (f.dtype != b->dtype) return PP_ERR_UNSUPPORTED;
     if (f.m != (transposed ? b->k : b->m) || f.k != (transposed ? b->m : b->k)) return PP_ERR_SHAPE;
-    return block_check_adapted(plan, n);
+    const pp_status_t st = block_check_adapted(plan, n);
+    if (st != PP_OK) return st;
+    return !b->on_device || f.device == b->device ? PP_OK : PP_ERR_DEVICE;
 }
 
 // ---- launches (everything has been checked) ----
@@ -115,7 +119,8 @@ pp_status_t launch_product(const pp_adapter_bank_t* b, bool of_b, const pp_block
     a.slot_elems = (of_b ? b->b_expand_slot : b->a_expand_slot) / 4;
     a.split_elems = split_elems;
     a.m = of_b ? b->m : b->k, a.n = n, a.splits = splits, a.rank_pad = b->rank_pad, a.relu = block_plan_facts(plan).relu;
-    hipLaunchKernelGGL(k8_expand_f32, dim3((unsigned)(((int64_t)a.m + 63) / 64), (unsigned)((n + 63) / 64)), dim3(256), 0, stream, a);
+    const int token_tiles = (n + 63) / 64;
+    hipLaunchKernelGGL(k8_expand_f32, dim3((unsigned)((a.m + 63) / 64), (unsigned)(token_tiles < 32768 ? token_tiles : 32768)), dim3(256), 0, stream, a);
     return PP_OK;
 }
 
@@ -136,6 +141,7 @@ pp_status_t pp_adapter_plan(const pp_adapter_desc_t* desc, pp_adapter_bank_t** o
     if (out_bank) *out_bank = nullptr;
     if (!desc || !out_bank) return PP_ERR_NULL;
     if (desc->m < 1 || desc->k < 1 || (int64_t)desc->m * desc->k >= ((int64_t)1 << 31)) return PP_ERR_SHAPE;
+    if (desc->m > kAdapterMaxRows || desc->k > kAdapterMaxRows) return PP_ERR_SHAPE;
     if (desc->slots < 1 || desc->slots > kAdapterMaxSlots || desc->max_rank < 1 || desc->max_rank > kAdapterMaxRank) return PP_ERR_SHAPE;
     if (desc->dtype != PP_F32 && desc->dtype != PP_F16) return PP_ERR_UNSUPPORTED;
     if (desc->flags & ~(uint32_t)PP_FLAG_HOST_ONLY) return PP_ERR_UNSUPPORTED;
@@ -177,6 +183,7 @@ pp_status_t pp_adapter_plan(const pp_adapter_desc_t* desc, pp_adapter_bank_t** o
 pp_status_t pp_adapter_load(pp_adapter_bank_t* bank, int32_t slot, int32_t rank, float scale, const void* a_dev, const void* b_dev, void* hip_stream) {
     if (!bank || (rank != 0 && (!a_dev || !b_dev))) return PP_ERR_NULL;
     if (slot < 0 || slot >= bank->slots || rank < 0 || rank > bank->max_rank) return PP_ERR_SHAPE;
+    if (!std::isfinite(scale)) return PP_ERR_UNSUPPORTED;
     if (rank && (misaligned(a_dev) || misaligned(b_dev))) return PP_ERR_ALIGN;
     const pp_status_t st = ready(bank);
     if (st != PP_OK) return st;
@@ -207,7 +214,7 @@ int64_t pp_adapter_work_bytes(const pp_adapter_bank_t* bank, int32_t n, int32_t 
 pp_status_t pp_adapter_project(const pp_adapter_bank_t* bank, const void* x_dev, const int32_t* slot_of_dev, void* u_dev, int32_t n, void* hip_stream) {
     if (!bank || !x_dev || !slot_of_dev || !u_dev) return PP_ERR_NULL;
     if (!tokens_ok(bank, n)) return PP_ERR_SHAPE;
-    if (misaligned(x_dev) || misaligned(u_dev)) return PP_ERR_ALIGN;
+    if (misaligned(x_dev) || misaligned(u_dev) || misaligned4(slot_of_dev)) return PP_ERR_ALIGN;
     const Range x(x_dev, (int64_t)bank->k * n * elem(bank)), u(u_dev, pp_adapter_u_bytes(bank, n)), s(slot_of_dev, (int64_t)n * 4);
     if (overlap(u, x) || overlap(u, s)) return PP_ERR_ALIGN;
     const pp_status_t st = ready(bank);
@@ -221,7 +228,7 @@ pp_status_t pp_adapter_run(const pp_adapter_bank_t* bank, const pp_block_gemm_pl
                            void* y_dev, int32_t n, void* hip_stream) {
     if (!bank || !plan || !x_dev || !slot_of_dev || !u_dev || !y_dev) return PP_ERR_NULL;
     if (!tokens_ok(bank, n)) return PP_ERR_SHAPE;
-    if (misaligned(x_dev) || misaligned(u_dev) || misaligned(y_dev)) return PP_ERR_ALIGN;
+    if (misaligned(x_dev) || misaligned(u_dev) || misaligned(y_dev) || misaligned4(slot_of_dev)) return PP_ERR_ALIGN;
     const Range x(x_dev, (int64_t)bank->k * n * elem(bank)), y(y_dev, (int64_t)bank->m * n * elem(bank)), u(u_dev, pp_adapter_u_bytes(bank, n)),
         s(slot_of_dev, (int64_t)n * 4);
     if (overlap(u, x) || overlap(u, s) || overlap(y, x) || overlap(y, u) || overlap(y, s)) return PP_ERR_ALIGN;
@@ -241,7 +248,7 @@ pp_status_t pp_adapter_grad_input(const pp_adapter_bank_t* bank, const pp_block_
                                   const int32_t* slot_of_dev, void* v_dev, void* dx_dev, int32_t n, void* hip_stream) {
     if (!bank || !dy_dev || !slot_of_dev || !v_dev || (gate_dev && !g_dev) || (dx_dev && !plan_t)) return PP_ERR_NULL;
     if (!tokens_ok(bank, n)) return PP_ERR_SHAPE;
-    if (misaligned(dy_dev) || misaligned(v_dev) || (gate_dev && (misaligned(gate_dev) || misaligned(g_dev))) || (dx_dev && misaligned(dx_dev))) return PP_ERR_ALIGN;
+    if (misaligned(dy_dev) || misaligned(v_dev) || misaligned4(slot_of_dev) || (gate_dev && (misaligned(gate_dev) || misaligned(g_dev))) || (dx_dev && misaligned(dx_dev))) return PP_ERR_ALIGN;
     const int64_t out_bytes = (int64_t)bank->m * n * elem(bank);
     const Range dy(dy_dev, out_bytes), v(v_dev, pp_adapter_v_bytes(bank, n)), s(slot_of_dev, (int64_t)n * 4);
     if (overlap(v, dy) || overlap(v, s)) return PP_ERR_ALIGN;
@@ -277,6 +284,7 @@ pp_status_t pp_adapter_grad_weights(const pp_adapter_bank_t* bank, const void* x
     const void* all[] = {x_dev, u_dev, g_dev, v_dev, da_dev, db_dev, work_dev};
     for (const void* p : all)
         if (misaligned(p)) return PP_ERR_ALIGN;
+    if (misaligned4(slot_of_dev) || misaligned4(which_dev)) return PP_ERR_ALIGN;
     const Range in[] = {Range(x_dev, x_is_act8 ? act8_bytes(bank->k, n) : (int64_t)bank->k * n * elem(bank)), Range(u_dev, pp_adapter_u_bytes(bank, n)),
                         Range(g_dev, (int64_t)bank->m * n * elem(bank)), Range(v_dev, pp_adapter_v_bytes(bank, n)), Range(slot_of_dev, (int64_t)n * 4),
                         Range(which_dev, (int64_t)count * 4)};

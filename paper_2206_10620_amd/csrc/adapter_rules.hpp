@@ -9,7 +9,8 @@ namespace ppc {
 constexpr int kAct8Block = 128;                 // columns that share a scale
 constexpr int kAdapterMaxRank = 128;
 constexpr int kAdapterMaxSlots = 65536;
-constexpr int kAdapterMaxTokens = 1 << 22;      // keeps every grid below 2^32 threads
+constexpr int kAdapterMaxTokens = 1 << 22;      // these two keep every grid below 2^32 threads
+constexpr int kAdapterMaxRows = 1 << 22;
 
 inline int64_t act8_pitch(int64_t n) { return (n + kAct8Block - 1) / kAct8Block * kAct8Block; }
 inline int64_t act8_scale_pitch(int64_t rows) { return (rows + 15) / 16 * 16; }

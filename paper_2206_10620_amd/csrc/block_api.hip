@@ -12,6 +12,7 @@
 struct pp_block_gemm_plan {
     ppc::BlockHostPlan hp;
     bool on_device = false;
+    int device = 0;
     void* d_apk = nullptr;
     float* d_bias = nullptr;
     int32_t* d_tile_off = nullptr;
@@ -175,7 +176,7 @@ static pp_status_t launch_lists(const pp_block_gemm_plan_t* plan, const void* x_
 namespace ppc {
 
 BlockPlanFacts block_plan_facts(const pp_block_gemm_plan_t* plan) {
-    return {plan->hp.m, plan->hp.k, plan->hp.dtype, (plan->hp.flags & PP_FLAG_RELU) ? 1 : 0};
+    return {plan->hp.m, plan->hp.k, plan->hp.dtype, (plan->hp.flags & PP_FLAG_RELU) ? 1 : 0, plan->device};
 }
 
 pp_status_t block_check_adapted(const pp_block_gemm_plan_t* plan, int32_t n) {
@@ -213,7 +214,8 @@ static pp_status_t make_plan(const pp_block_gemm_desc_t* desc, bool transposed, 
     }
     if (!(desc->flags & PP_FLAG_HOST_ONLY)) {
         const BlockHostPlan& hp = p->hp;
-        bool ok = put(&p->d_apk, hp.apk.data(), hp.apk.size() * sizeof(uint16_t));
+        bool ok = hipGetDevice(&p->device) == hipSuccess;
+        ok = ok && put(&p->d_apk, hp.apk.data(), hp.apk.size() * sizeof(uint16_t));
         ok = ok && put(&p->d_bias, hp.bias.data(), hp.bias.size() * sizeof(float));
         ok = ok && put(&p->d_tile_off, hp.tile_off.data(), hp.tile_off.size() * sizeof(int32_t));
         ok = ok && put(&p->d_tile_cols, hp.tile_cols.data(), hp.tile_cols.size() * sizeof(int32_t), 256 * sizeof(int32_t));   // the kernels read ahead: a chunk, or two segments of 128

@@ -57,7 +57,7 @@ struct K4Expand;
 // What the adapters need of a product: its sizes (PP_ERR_UNSUPPORTED for a host-only plan or a forced variant that does not take n),
 // and its launch, with the adapters' part added before act (binary16), or without act, which whoever adds them applies (binary32).
 struct BlockPlanFacts {
-    int m, k, dtype, relu;
+    int m, k, dtype, relu, device;
 };
 BlockPlanFacts block_plan_facts(const pp_block_gemm_plan_t* plan);
 pp_status_t block_check_adapted(const pp_block_gemm_plan_t* plan, int32_t n);

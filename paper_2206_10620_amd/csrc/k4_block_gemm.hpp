@@ -102,7 +102,7 @@ __device__ __forceinline__ void k4_wait_vm(int n) {
 
 // RAGGED: n is not a multiple of 8 (a variant of its own: the checks cost the aligned case 5 %, 66.5 -> 70 us on 4096 columns)
 template <bool RAGGED, typename Args = K4Args>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, std::is_same<Args, K4Args>::value ? 2 : 8))) void k4_block_gemm(const Args a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void k4_block_gemm(const Args a) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char k4_smem[];
     constexpr int NS = kK4Stages, NT = 4;
     const int lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
@@ -162,9 +162,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, std::is_
     };
 
     // accumulators: register i of tile (mt, nt) is row mt * 32 + (i / 4) * 8 + (lane / 32) * 4 + i % 4, column nt * 32 + lane % 32
-    constexpr bool kAdapted = std::is_same<Args, K4AdaptedArgs>::value;
     k4_f16 acc[2][NT];
-    auto add_bias = [&](bool first) {
+    constexpr bool kAdapted = std::is_same<Args, K4AdaptedArgs>::value;
+    if constexpr (!kAdapted) {
         const float* b = a.bias + rt * kBlockRowTile + (lane >> 5) * 4;
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt)
@@ -172,10 +172,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, std::is_
             for (int i = 0; i < 16; ++i) {
                 const float bv = b[mt * 32 + (i >> 2) * 8 + (i & 3)];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) acc[mt][nt][i] = first ? bv : acc[mt][nt][i] + bv;
+                for (int nt = 0; nt < NT; ++nt) acc[mt][nt][i] = bv;
             }
-    };
-    if constexpr (!kAdapted) add_bias(true);
+    }
 
     // transposing read: inside a block of 16 lanes, lane 4 j + q reads four columns of list entry j; the
     // result hands lane i column i of entries 0..3.  Blocks 0, 1 take columns 0-15, 16-31 of entries
@@ -226,21 +225,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, std::is_
     };
 
     fetch_rows();
-    if (nch > 0) {
+    if (kAdapted || nch > 0) {                 // (an empty list: nothing is issued, awaited or multiplied)
 #pragma unroll
         for (int c = 0; c < NS; ++c)
             if (c < nch) issue(c, c);
-    }
-    // while the first chunks are on their way
-    if constexpr (kAdapted) {
+        if constexpr (kAdapted) {                                // while the first chunks are on their way
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
+            for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = k4_f16(0.0f);
-        k4_expand<NT>(a.expand, acc, col0 + wave * 128, a.n, rt, lane, 0, 1);
-        add_bias(false);
-    }
-    if (nch > 0) {
+                for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = k4_f16(0.0f);
+            k4_expand<NT>(a.expand, acc, col0 + wave * 128, a.n, rt, lane, 0, 1);
+            const float* b = a.bias + rt * kBlockRowTile + (lane >> 5) * 4;
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float bv = b[mt * 32 + (i >> 2) * 8 + (i & 3)];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) acc[mt][nt][i] += bv;
+                }
+        }
         k4_wait_vm(RAGGED && drain ? 0 : (nch > NS ? NS - 1 : nch - 1) * (wload ? 5 : 4));
         __syncthreads();
         read_frags(0, 0);

@@ -252,10 +252,10 @@ struct K8Expand {
     int64_t slot_elems, split_elems;
     int32_t m, n, splits, rank_pad, relu;
 };
-__global__ __launch_bounds__(256) void k8_expand_f32(const K8Expand a) {
+__device__ __forceinline__ void k8_expand_tile(const K8Expand& a, int token_tile) {
     const int lane = (int)(threadIdx.x & 63u), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int c = lane & 15, g = lane >> 4;
-    const int row0 = ((int)blockIdx.x * 4 + wave) * 16, t0 = (int)blockIdx.y * 64 + c * 4, left = a.n - t0;
+    const int row0 = ((int)blockIdx.x * 4 + wave) * 16, t0 = token_tile * 64 + c * 4, left = a.n - t0;
     if (row0 >= a.m) return;
     KxToken tok[4];
     bool any = false;
@@ -314,6 +314,9 @@ __global__ __launch_bounds__(256) void k8_expand_f32(const K8Expand a) {
             if (a.relu) y[i][f] = y[i][f] > 0.0f ? y[i][f] : 0.0f;
         k8_store<float, 4>(a.y + (int64_t)(row0 + 4 * g + i) * a.n + t0, row0 + 4 * g + i < a.m ? left : 0, y[i]);
     }
+}
+__global__ __launch_bounds__(256) void k8_expand_f32(const K8Expand a) {
+    for (int tile = (int)blockIdx.y; tile * 64 < a.n; tile += (int)gridDim.y) k8_expand_tile(a, tile);
 }
 
 // ---- gradients of A and B ----

@@ -20,7 +20,8 @@ def bank(m=64, k=32, slots=4, max_rank=8, dtype=pp.PP_F16, flags=H):
 
 
 def test_bank_refusals():
-    for bad in (dict(m=0), dict(k=0), dict(m=1 << 16, k=1 << 15), dict(slots=0), dict(slots=65537), dict(max_rank=0), dict(max_rank=129)):
+    for bad in (dict(m=0), dict(k=0), dict(m=1 << 16, k=1 << 15), dict(slots=0), dict(slots=65537), dict(max_rank=0), dict(max_rank=129),
+                dict(m=(1 << 22) + 1, k=1), dict(m=1, k=(1 << 22) + 1)):
         assert bank(**bad)[0] == pp.PP_ERR_SHAPE, bad
     assert bank(dtype=2)[0] == pp.PP_ERR_UNSUPPORTED
     assert bank(flags=H | pp.PP_FLAG_RELU)[0] == pp.PP_ERR_UNSUPPORTED
@@ -47,6 +48,8 @@ def test_load_refusals(small):
     assert pp.pp_adapter_load(h, 0, 1, 1.0, 16, 0) == pp.PP_ERR_NULL
     for slot, rank in ((-1, 1), (4, 1), (0, -1), (0, 9)):
         assert pp.pp_adapter_load(h, slot, rank, 1.0, 16, 32) == pp.PP_ERR_SHAPE
+    for scale in (float("inf"), float("-inf"), float("nan")):
+        assert pp.pp_adapter_load(h, 0, 1, scale, 16, 32) == pp.PP_ERR_UNSUPPORTED
     assert pp.pp_adapter_load(h, 0, 1, 1.0, 18, 32) == pp.PP_ERR_ALIGN
     assert pp.pp_adapter_load(h, 0, 1, 1.0, 16, 40) == pp.PP_ERR_ALIGN
     assert pp.pp_adapter_load(h, 0, 0, 1.0, 0, 0) == pp.PP_ERR_UNSUPPORTED         # all in order, but the bank is host-only
@@ -63,8 +66,9 @@ def test_run_refusals(small):
     for name in ("x", "u", "y"):
         assert run(**{name: a[7] + 8}) == pp.PP_ERR_ALIGN, name
     assert run(y=a[0]) == run(y=a[0] + 16) == run(u=a[0]) == run(u=a[1]) == run(y=a[1]) == run(u=a[3]) == pp.PP_ERR_ALIGN
+    assert run(s=a[7] + 2) == pp.PP_ERR_ALIGN
     assert run(plan=plan_t.handle) == pp.PP_ERR_SHAPE
-    assert run() == pp.PP_ERR_UNSUPPORTED
+    assert run(s=a[7] + 4) == run() == pp.PP_ERR_UNSUPPORTED
     other = synth.random_block_layer("a", 64, 32, 8, 16, 16, "f32", 0.5, 0.5, 3)
     p32 = pp.block_plan_from_layer(other, host_only=True)
     assert run(plan=p32.handle) == pp.PP_ERR_UNSUPPORTED                           # another storage type
@@ -72,7 +76,7 @@ def test_run_refusals(small):
     project = lambda **kw: pp.pp_adapter_project(*{**dict(bank=h, x=a[0], s=a[1], u=a[2], n=8), **kw}.values())
     for name in ("bank", "x", "s", "u"):
         assert project(**{name: None}) == pp.PP_ERR_NULL, name
-    assert project(n=0) == pp.PP_ERR_SHAPE and project(u=a[0]) == project(x=a[0] + 2) == pp.PP_ERR_ALIGN and project() == pp.PP_ERR_UNSUPPORTED
+    assert project(n=0) == pp.PP_ERR_SHAPE and project(s=a[1] + 1) == project(u=a[0]) == project(x=a[0] + 2) == pp.PP_ERR_ALIGN and project() == pp.PP_ERR_UNSUPPORTED
 
 
 def test_gradient_refusals(small):
@@ -86,6 +90,7 @@ def test_gradient_refusals(small):
         assert gi(**{name: a[9] + 4}) == pp.PP_ERR_ALIGN, name
     for kw in (dict(v=a[0]), dict(v=a[1]), dict(v=a[2]), dict(dx=a[0]), dict(dx=a[1]), dict(dx=a[2]), dict(dx=a[4]), dict(g=a[0] + 16), dict(g=a[1]), dict(v=a[3]), dict(dx=a[3])):
         assert gi(**kw) == pp.PP_ERR_ALIGN, kw
+    assert gi(s=a[3] + 2) == pp.PP_ERR_ALIGN
     # in place, without a gate, without dx: in order but for the host-only bank
     assert gi(g=a[0]) == gi(gate=None, g=None) == gi(plan=None, dx=None) == pp.PP_ERR_UNSUPPORTED
     gw = lambda **kw: pp.pp_adapter_grad_weights(*{**dict(bank=h, x=a[0], held=0, u=a[1], g=a[2], v=a[3], s=a[4], which=a[5], count=2, da=a[6], db=a[7], work=a[8],
@@ -98,6 +103,7 @@ def test_gradient_refusals(small):
     for out in ("da", "db", "work"):
         for other in range(6):
             assert gw(**{out: a[other]}) == pp.PP_ERR_ALIGN, (out, other)
+    assert gw(s=a[4] + 2) == gw(which=a[5] + 1) == pp.PP_ERR_ALIGN
     assert gw(db=a[6]) == gw(work=a[7]) == pp.PP_ERR_ALIGN
     assert gw() == gw(held=1) == pp.PP_ERR_UNSUPPORTED
 

@@ -38,11 +38,13 @@ def test_borders():
                 [np.finfo(dtype).tiny, 1e-7, -6e-8, 0, 0, 0], [np.finfo(dtype).smallest_subnormal, 0, 0, 0, 0, 0], [65024, -65024, 512, 1, 0, 0]]
         x = np.array(rows, dtype)
         assert np.array_equal(round_trip(x)[1], held8(x).astype(dtype))
-    x = np.array([[3.4e38, -1e38, 1.0], [1e-44, -1.2e-38, 0]], np.float32)
+    x = np.array([[3.3e38, -1e38, 1.0], [1e-44, -1.2e-38, 0]], np.float32)
     assert np.array_equal(round_trip(x)[1], held8(x).astype(np.float32))
     # values that only 8 bits round above binary16's largest come back as that
     x = np.array([[65504, -65504, 100]], np.float16)
     held, got = round_trip(x)
+    largest = np.finfo(np.float32).max
+    assert round_trip(np.array([[largest, -largest, 0]], np.float32))[1].tolist() == [[largest, -largest, 0]]
     assert got.tolist() == [[65504, -65504, 1024]] and held.unpack(pp.PP_F32).cpu().tolist() == [[65536, -65536, 1024]]
 
 
@@ -75,3 +77,17 @@ def test_on_a_stream_of_its_own():
     got = pp.act8_pack(x, stream=stream.cuda_stream).unpack(stream=stream.cuda_stream)
     stream.synchronize()
     assert np.array_equal(got.cpu().numpy(), held8(x.cpu().numpy()).astype(np.float32))
+
+
+def test_offsets_beyond_32_bits():
+    """2^31 - 256 values in rows of 4 MB and in one row; the ends are looked at."""
+    for rows, n in ((1 << 10, (1 << 21) - 1), (1, (1 << 31) - 256)):
+        print("case", rows, n, flush=True)
+        x = torch.zeros((rows, n), dtype=torch.float16, device="cuda")
+        x[-1, -300:] = torch.arange(300, device="cuda").half() - 150
+        x[0, :300] = torch.arange(300, device="cuda").half() - 150
+        got = pp.act8_pack(x).unpack()
+        for r, part in ((0, slice(0, 640)), (rows - 1, slice(n - 640 - n % 128, n))):
+            assert np.array_equal(got[r, part].cpu().numpy(), held8(x[r: r + 1, part].cpu().numpy()).astype(np.float16)[0])
+        assert int((got != 0).sum()) == int((x != 0).sum())
+        del x, got

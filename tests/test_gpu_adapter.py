@@ -193,6 +193,98 @@ def test_without_adapters_it_is_the_block_product():
         assert torch.equal(s.bank.run(s.plan, s.x, s.slot_of), s.plan.run(s.x))
 
 
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("keep", [0.0, 1.0])
+def test_nothing_and_all_of_the_layer_kept(dtype, keep):
+    """Empty column lists: the bias and the adapters alone; and a layer without a pruned weight."""
+    for n in (3, 130):
+        s = Setup(Problem(dtype, 100, 72, n, [16, 33], 40, "mixed", relu=True, keep=keep, seed=17))
+        s.check_forward()
+        s.check_backward(True, True)
+    s = Setup(Problem(dtype, 4096, 64, 4096, [4], 4, "runs", keep=keep, bm=64, bk=64, seed=18))       # the 512-column tile
+    s.check_forward()
+
+
+def test_padding_tokens_may_hold_anything():
+    """Tokens without an adapter, as a padded batch has them, filled with NaN and infinities: the others and all gradients are untouched."""
+    p = Problem("f16", 96, 130, 400, [16, 24], 24, "mixed", seed=19)
+    s = Setup(p)
+    y0 = s.bank.run(s.plan, s.x, s.slot_of)
+    g0, da0, db0 = s.step(held=True)
+    pad = p.slot_of < 0
+    p.x[:, pad], p.dy[:, pad] = np.nan, np.inf
+    s2 = Setup(p)
+    y = s2.bank.run(s2.plan, s2.x, s2.slot_of)
+    u = s2.bank.project(s2.x, s2.slot_of)
+    g = s2.bank.grad_input(s2.plan_t, s2.dy, s2.slot_of)
+    da, db = s2.bank.grad_weights(s2.x, u, g.g, g.v, s2.slot_of, dev(np.array([0, 1], np.int32)))
+    keep = torch.from_numpy(np.flatnonzero(~pad)).cuda()
+    _, da1, db1 = s.step()
+    assert torch.equal(y[:, keep], y0[:, keep]) and torch.equal(g.dx[:, keep], g0.dx[:, keep])
+    assert torch.equal(da, da1) and torch.equal(db, db1) and torch.equal(db, db0) and torch.isfinite(da0).all()
+
+
+@pytest.mark.parametrize("scale", [0.0, -1.5, 1e-30, 3e38])
+def test_factors(scale):
+    """A factor of zero, a negative one, the ends of binary32; with the largest B is zero, and so is the part it stands before."""
+    p = Problem("f32" if scale == 1e-30 else "f16", 64, 48, 40, [8], 8, "one", seed=20)
+    p.c[0] = float(np.float32(scale))
+    if scale > 1:
+        p.b[0][:] = 0
+    s = Setup(p)
+    s.check_forward()
+    if scale <= 1:
+        s.check_backward()
+
+
+def _far(dtype, k, n, m, last):
+    """A product whose x passes 2^32 bytes, adapters on its first and last tokens only; the reference takes those tokens alone."""
+    tdt = torch.float16 if dtype == "f16" else torch.float32
+    lay = Problem(dtype, m, k, 1, [8], 8, seed=21).layer
+    plan = pp.block_plan_from_layer(lay)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.empty((k, n), dtype=tdt, device="cuda")
+    for r in range(0, k, 64):
+        x[r:r + 64] = torch.randn((min(64, k - r), n), generator=gen, device="cuda").to(tdt)
+    slot_of = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    slot_of[:5] = 0
+    slot_of[n - last:] = 0
+    a, b = (torch.randn((8, k), generator=gen, device="cuda") / k ** 0.5).to(tdt), torch.randn((m, 8), generator=gen, device="cuda").to(tdt)
+    bank = pp.AdapterBank(m, k, 1, 8, pp.PP_F16 if dtype == "f16" else pp.PP_F32)
+    bank.load(0, a, b, 0.5)
+    print("case far", dtype, k, n, flush=True)
+    y, u = bank.run(plan, x, slot_of, keep=True)
+    plain = plan.run(x)
+    at = torch.cat([torch.arange(5), torch.arange(n - last, n)]).cuda()
+    xs = x[:, at].double()
+    wd = torch.from_numpy(np.where(lay.keep_matrix(), lay.weights, 0).astype(np.float32)).cuda().to(tdt).double()
+    want = wd @ xs + torch.from_numpy(lay.bias).cuda().double()[:, None] + 0.5 * (b.double() @ (a.double() @ xs))
+    size = wd.abs() @ xs.abs() + 0.5 * (b.abs().double() @ (a.abs().double() @ xs.abs())) + 1
+    half = 2.0 ** -11 if dtype == "f16" else 2.0 ** -24
+    assert bool(((y[:, at].double() - want).abs() <= half * want.abs() + (2 * k + 32) * 2.0 ** -24 * size).all())
+    y[:, at] = plain[:, at]
+    assert torch.equal(y, plain)
+    dy = torch.ones((m, n), dtype=tdt, device="cuda")
+    g = bank.grad_input(None, dy, slot_of)
+    which = torch.zeros(1, dtype=torch.int32, device="cuda")
+    da, db = bank.grad_weights(x, u, g.g, g.v, slot_of, which)
+    v = b.double().sum(0)
+    room = (2 * m + 2 * len(at) + 32) * 2.0 ** -24 * 0.5 * b.abs().double().sum(0)[:, None] * xs.abs().sum(1)[None]
+    assert bool(((da[0].double() - 0.5 * v[:, None] * xs.sum(1)[None]).abs() <= room).all())
+    us = a.double() @ xs
+    room = (2 * k + 2 * len(at) + 32) * 2.0 ** -24 * 0.5 * (a.abs().double() @ xs.abs()).sum(1)[None]
+    assert bool(((db[0].double() - 0.5 * us.sum(1)[None]).abs() <= room).all())
+    plan.close()
+
+
+def test_offsets_beyond_32_bits_f16():
+    _far("f16", 500, (1 << 22) - 1, 8, 300)
+
+
+def test_offsets_beyond_32_bits_f32():
+    _far("f32", 260, 1 << 22, 8, 129)
+
+
 def test_equal_calls_give_equal_bits():
     s = Setup(Problem("f16", 256, 512, 700, [16, 33], 40, "mixed", seed=11))
     a, b = s.step(), s.step()

@@ -354,6 +354,7 @@ struct K8Turn {
     const int32_t* rank;
     const float* scale;
     int32_t n, slots, blocks, rank_pad, splits[2];
+    int32_t x_is_act8;          // v's tokens in the order in which lanes take 32 bytes of x: see k8_grad
 };
 
 // A workgroup turns a block of a rank tile of v or u for one slot, a wavefront four of its ranks: lane 4 q + j has tokens 8 q .. of rank j.
@@ -389,7 +390,9 @@ template <typename T> __global__ __launch_bounds__(256) void k8_turn(const K8Tur
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = (byte >> i) & 1u ? v[i] : 0.0f;
     const int64_t part_of = ((int64_t)at * 2 + side) * a.blocks + b;
-    k8_v8<T>* dst = static_cast<k8_v8<T>*>(a.out.w) + ((part_of * tiles_all + r) * 4 + (q >> 2)) * PARTS * 64 + (q & 3) * 16 + wave * 4 + j4;
+    const bool swapped = side == 0 && a.x_is_act8;
+    const int step = swapped ? q & 3 : q >> 2, quarter = swapped ? q >> 2 : q & 3;       // of the 16 x 16 x 32 products; lanes of one
+    k8_v8<T>* dst = static_cast<k8_v8<T>*>(a.out.w) + ((part_of * tiles_all + r) * 4 + step) * PARTS * 64 + quarter * 16 + wave * 4 + j4;
     if constexpr (half) {
         uint32_t top = 0;
 #pragma unroll
@@ -490,7 +493,7 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
         };
 
         k8_any<T, 8> z[RW][4];                                   // on its way: the next block's
-        uint2 z8[RW][4];
+        uint4 z8[RW][2];
         uint32_t zs[RW];
         auto load_z = [&](int b) {
             const int tb = b * 128;
@@ -499,12 +502,10 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
                 const int row = row0 + i * 16 + c;
                 const bool row_ok = row < rows;
                 if (HELD8 && of_a) {
-                    const int8_t* src = static_cast<const int8_t*>(a.x) + (int64_t)row * a.x_pitch + tb + g * 8;
-#pragma unroll
-                    for (int st = 0; st < 4; ++st) {
-                        z8[i][st] = uint2{0u, 0u};
-                        if (row_ok) z8[i][st] = *reinterpret_cast<const uint2*>(src + st * 32);
-                    }
+                    // 32 bytes of a row to a lane: product st takes tokens 32 g + 8 st .., not 32 st + 8 g .. as otherwise
+                    const uint4* src = reinterpret_cast<const uint4*>(static_cast<const int8_t*>(a.x) + (int64_t)row * a.x_pitch + tb + g * 32);
+                    z8[i][0] = z8[i][1] = uint4{0u, 0u, 0u, 0u};
+                    if (row_ok) z8[i][0] = src[0], z8[i][1] = src[1];
                     const int r4 = row0 + i * 16 + 4 * g;
                     zs[i] = 0;
                     if (r4 < a.x_scale_pitch) zs[i] = *reinterpret_cast<const uint32_t*>(a.x_scale + (int64_t)b * a.x_scale_pitch + r4);
@@ -543,13 +544,17 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
                 for (int st = 0; st < 4; ++st) {
                     if (HELD8 && of_a) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) cur[i][st][e] = (T)(float)(int8_t)((e < 4 ? z8[i][st].x : z8[i][st].y) >> (8 * (e & 3)));
+                        for (int e = 0; e < 8; ++e) {
+                            const uint4 w = z8[i][st >> 1];
+                            cur[i][st][e] = (T)(float)(int8_t)((st & 1 ? (e < 4 ? w.z : w.w) : (e < 4 ? w.x : w.y)) >> (8 * (e & 3)));
+                        }
                     } else {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) cur[i][st][e] = z[i][st][e];
                     }
                     if (!whole) {                                // tokens of other slots: whatever z holds there, not a number even
-                        const uint32_t byte = (uint32_t)((st < 2 ? m0 : m1) >> (32 * (st & 1) + 8 * g)) & 0xffu;
+                        const int of = HELD8 && of_a ? g * 4 + st : st * 4 + g;           // eighth of the block, of sixteen
+                        const uint32_t byte = (uint32_t)((of < 8 ? m0 : m1) >> (8 * (of & 7))) & 0xffu;
 #pragma unroll
                         for (int e = 0; e < 8; ++e) cur[i][st][e] = (byte >> e) & 1u ? cur[i][st][e] : (T)0.0f;
                     }

@@ -19,7 +19,7 @@
  * slot's matrices does stays with that token, with that slot's tokens and with that slot's gradients.
  *
  * Storage is the bank's dtype for x, y, dy, g, dx, A and B; sums, u, v and the gradients of A and B are binary32.  In a
- * PP_F16 bank u and v enter products as two binary16 parts with a power of two taken out, which leaves them 22 bits.
+ * PP_F16 bank u and v enter products as two binary16 parts with a power of two taken out, which leaves them 20 bits or more.
  *
  * Pointers named *_dev are device pointers to the device the bank was made on, which has to be current, and the plan's
  * (PP_ERR_DEVICE otherwise).  Matrices are row-major without gaps and 16-byte aligned, lists of

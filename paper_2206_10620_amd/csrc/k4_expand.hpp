@@ -1,10 +1,12 @@
 // The adapters' part of a block product in binary16 (include/pp_adapter.h): c_s B_s u added to the accumulators of a wavefront
 // before the product's own sum, so that it meets the sum, the bias and the activation in fp32.
 //
-// u [split][token][rank] is in fp32 and far smaller than x.  A lane of the matrix instruction's second operand holds eight
-// consecutive ranks of one token, which is how u lies in memory: no staging.  They enter as two binary16 parts, hi and lo, after
-// a power of two that brings the token's largest |u| to [2^14, 2^15) is taken out: 22 bits, whatever the size of u.  B lies in
-// operand order, 1 KB per 32 rows and 16 ranks.
+// u is in fp32 and far smaller than x.  A lane of the matrix instruction's second operand holds eight consecutive ranks of one token,
+// which is how u lies in memory: no staging.  They enter as two binary16 parts, hi and lo, after a power of two that brings the
+// token's largest |u| of 16 ranks to [2^14, 2^15) is taken out: 20 bits, whatever the size of u, where y keeps 11.  B lies in operand
+// order, 1 KB per 32 rows and 16 ranks.
+// What it costs is reading u, once for every 64 rows of y: 4096 x 1024 at 0.17 on 2048 tokens takes 17 us without adapters, 5, 7, 13 and
+// 24 more with rank 16, 32, 64 and 128 (two shares of u, 8 bytes a token and rank, are four times a row of x).
 //
 // The tokens of a wavefront are taken slot by slot.  A matrix instruction computes all its columns with the one slot's B;
 // only the columns of that slot's tokens are taken over, so nothing a slot holds can reach another slot's tokens.
@@ -62,7 +64,7 @@ __device__ __forceinline__ float kx_pow2(int e) { return __builtin_bit_cast(floa
 typedef __fp16 kx_p2 __attribute__((ext_vector_type(2)));
 typedef _Float16 kx_h2 __attribute__((ext_vector_type(2)));
 
-// Eight fp32 values as two binary16 parts, v * 2^shift = hi + lo up to 2^-21 of it (or 2^-24 of the token's largest), and the
+// Eight fp32 values as two binary16 parts, v * 2^shift = hi + lo up to 2^-20 of it (or 2^-38 of the token's largest), and the
 // factor that undoes the shift.  Both parts are cut, not rounded: what hi leaves, lo takes.  A lane holds half of its token's values,
 // lane ^ 32 the other.  An infinity or a NaN is hi alone, and the shift that of the token's other values.
 template <int G> __device__ __forceinline__ void kx_split(const float (&v)[G][8], kx_h8 (&hi)[G], kx_h8 (&lo)[G], float& down) {

@@ -135,26 +135,40 @@ __global__ __launch_bounds__(64 * kProjectWaves) void k8_project(const K8Project
     float* u = a.u + split * kx_share(a.n, a.rank_pad);
 
     typedef k8_any<T, FT> Piece;
-    auto load = [&](int st, Piece (&v)[8], bool write_g) {
+    // Rows of a step.  WHOLE: all are there, and all tokens of the tile; no branch stands between the loads then, which would make
+    // the wait for one a wait for all.
+    auto load = [&](auto whole, auto write_g, int st, Piece (&v)[8]) {
+        constexpr bool WHOLE = decltype(whole)::value;
         const int row0 = st * 32 + g * 8;
         const T* src = x + (int64_t)row0 * a.n + mine0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = k8_load<T, FT>(src + (int64_t)i * a.n, row0 + i < a.rows ? left : 0);
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (WHOLE) v[i] = *reinterpret_cast<const Piece*>(src + (int64_t)i * a.n);
+            else v[i] = k8_load<T, FT>(src + (int64_t)i * a.n, row0 + i < a.rows ? left : 0);
+        }
         if constexpr (GATED) {
-            k8_any<int8_t, FT> q[8];
+            typedef k8_any<int8_t, FT> Gate;
+            Gate q[8];
             const int8_t* gate = a.gate + (int64_t)row0 * a.gate_pitch + mine0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q[i] = k8_load<int8_t, FT>(gate + i * a.gate_pitch, row0 + i < a.rows && left > 0 ? FT : 0);
+            for (int i = 0; i < 8; ++i) {
+                if constexpr (WHOLE) q[i] = *reinterpret_cast<const Gate*>(gate + i * a.gate_pitch);
+                else q[i] = k8_load<int8_t, FT>(gate + i * a.gate_pitch, row0 + i < a.rows && left > 0 ? FT : 0);
+            }
             T* dst = static_cast<T*>(a.g) + (int64_t)row0 * a.n + mine0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
 #pragma unroll
                 for (int f = 0; f < FT; ++f)
-                    if (!(k8_at<k8_any<int8_t, FT>, int8_t>(q[i], f) > 0)) k8_put(v[i], f, (T)0.0f);
-                if (write_g && row0 + i < a.rows) k8_store<T, FT>(dst + (int64_t)i * a.n, left, v[i]);
+                    if (!(k8_at<Gate, int8_t>(q[i], f) > 0)) k8_put(v[i], f, (T)0.0f);
+                if constexpr (decltype(write_g)::value) {
+                    if constexpr (WHOLE) *reinterpret_cast<Piece*>(dst + (int64_t)i * a.n) = v[i];
+                    else if (row0 + i < a.rows) k8_store<T, FT>(dst + (int64_t)i * a.n, left, v[i]);
+                }
             }
         }
     };
+    const bool whole_here = t0 + 16 * FT <= a.n && w1 * 32 <= a.rows;
 
     // One slot's tokens (slot -1: only the gate), ranks from tile rt0 on.
     auto pass = [&](int slot, int rt0, int tiles, bool is_first) {
@@ -163,28 +177,48 @@ __global__ __launch_bounds__(64 * kProjectWaves) void k8_project(const K8Project
         for (int r = 0; r < RG; ++r)
 #pragma unroll
             for (int f = 0; f < FT; ++f) acc[r][f] = k8_f4(0.0f);
-        const bool write_g = GATED && is_first && blockIdx.y == 0;
         const T* ops = static_cast<const T*>(a.operands) + (slot < 0 ? 0 : slot * a.slot_elems) + (int64_t)rt0 * a.steps * 512 + lane * 8;
-        Piece v[8];
-        if (w0 < w1) load(w0, v, write_g);
-        for (int st = w0; st < w1; ++st) {
-            Piece next[8];
+        // the next step's rows are on their way while this one's are multiplied
+        auto steps = [&](auto whole, auto write_g) {
+            Piece v[8], next[8];
             k8_v8<T> op[RG];
-#pragma unroll
-            for (int r = 0; r < RG; ++r)
-                if (r < tiles) op[r] = *reinterpret_cast<const k8_v8<T>*>(ops + ((int64_t)r * a.steps + st) * 512);
-            if (st + 1 < w1) load(st + 1, next, write_g);
-#pragma unroll
-            for (int f = 0; f < FT; ++f) {
-                k8_v8<T> b;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) b[i] = k8_at<Piece, T>(v[i], f);
+            auto load_ops = [&](int st) {
 #pragma unroll
                 for (int r = 0; r < RG; ++r)
-                    if (r < tiles) acc[r][f] = k8_mfma(op[r], b, acc[r][f]);
-            }
+                    op[r] = *reinterpret_cast<const k8_v8<T>*>(ops + ((int64_t)(r < tiles ? r : 0) * a.steps + st) * 512);
+            };
+            auto multiply = [&]() {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = next[i];
+                for (int f = 0; f < FT; ++f) {
+                    k8_v8<T> b;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) b[i] = k8_at<Piece, T>(v[i], f);
+#pragma unroll
+                    for (int r = 0; r < RG; ++r)
+                        if (r < tiles) acc[r][f] = k8_mfma(op[r], b, acc[r][f]);
+                }
+            };
+            load(whole, write_g, w0, v);
+            for (int st = w0; st + 1 < w1; ++st) {
+                load_ops(st);
+                load(whole, write_g, st + 1, next);
+                multiply();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = next[i];
+            }
+            load_ops(w1 - 1);
+            multiply();
+        };
+        if (w0 < w1) {
+            const std::true_type yes;
+            const std::false_type no;
+            if (GATED && is_first && blockIdx.y == 0) {
+                if (whole_here) steps(yes, std::integral_constant<bool, GATED>{});
+                else steps(no, std::integral_constant<bool, GATED>{});
+            } else {
+                if (whole_here) steps(yes, no);
+                else steps(no, no);
+            }
         }
         if (slot < 0) return;
         const int rank = a.rank[slot];
@@ -447,8 +481,6 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
     const int row0 = ((int)blockIdx.x - (of_a ? 0 : a.tiles_k)) * 64 * RW + wave * 16 * RW;
     if (row0 >= rows) return;
     const int at = (int)blockIdx.y, split = (int)blockIdx.z;
-    const K8Slot slot = a.in.slots[at];
-    const int rank = __builtin_amdgcn_readfirstlane(slot.rank);
     const int tiles_all = a.rank_pad / 16;
     const K8Mask* masks = a.in.masks + (int64_t)at * a.blocks;
 
@@ -460,10 +492,13 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
         return (uint64_t)__builtin_amdgcn_ballot_w64(some);
     };
     const int groups = (a.blocks + 63) / 64;
+    const uint64_t found0 = found(0);                            // does not wait for the rank
+    const K8Slot slot = a.in.slots[at];
+    const int rank = __builtin_amdgcn_readfirstlane(slot.rank);
     int mine = 0, skip = 0;                                      // this workgroup's share of the blocks found
     if (rank > 0) {
-        int count = 0;
-        for (int i = 0; i < groups; ++i) count += __builtin_popcountll(found(i));
+        int count = __builtin_popcountll(found0);
+        for (int i = 1; i < groups; ++i) count += __builtin_popcountll(found(i));
         skip = (int)((int64_t)count * split / a.splits);
         mine = (int)((int64_t)count * (split + 1) / a.splits) - skip;
     }
@@ -481,7 +516,7 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
         uint64_t left = 0;
         if (todo > 0) {
             int over = skip;
-            left = found(0);
+            left = found0;
             while (__builtin_popcountll(left) <= over) over -= __builtin_popcountll(left), left = found(++group);
             for (; over > 0; --over) left &= left - 1;
         }
@@ -519,7 +554,8 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
 
         int b = 0;
         if (todo > 0) b = next_block(), load_z(b);
-        for (int done = 0; done < todo; ++done) {
+        // (the last block has no next one: were that a condition, the wait for w would be one for the next z too)
+        auto block = [&](auto last) {
             const int64_t part_of = ((int64_t)at * 2 + (of_a ? 0 : 1)) * a.blocks + b;
             const k8_v8<T>* ops = static_cast<const k8_v8<T>*>(a.in.w) + (part_of * tiles_all + rt0) * 4 * PARTS * 64 + lane;
             const float* downs = a.in.down + part_of * a.rank_pad + rt0 * 16 + c;
@@ -565,7 +601,7 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
                     scales[i][e] = HELD8 && of_a ? __builtin_bit_cast(float, s == 255u ? 0x7fc00000u : s << 23) : 1.0f;
                 }
             }
-            if (done + 1 < todo) b = next_block(), load_z(b);
+            if constexpr (!decltype(last)::value) b = next_block(), load_z(b);
 #pragma unroll
             for (int r = 0; r < RG; ++r)
                 if (r < tiles) {
@@ -584,7 +620,9 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) acc[i][r][e] = __builtin_fmaf(sum[i][e] * down[r & 1], scales[i][e], acc[i][r][e]);
                 }
-        }
+        };
+        for (int done = 0; done + 1 < todo; ++done) block(std::false_type{});
+        if (todo > 0) block(std::true_type{});
         // lane's results: rows 4 g + e, rank c
 #pragma unroll
         for (int i = 0; i < RW; ++i)

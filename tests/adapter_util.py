@@ -56,7 +56,7 @@ class Problem:
             size[:, t] += abs(self.c[s]) * (np.abs(b) @ (np.abs(a) @ np.abs(x[:, t])))
         if self.relu:
             y = np.maximum(y, 0.0)
-        # every product and sum in binary32, in any order: k + rank terms, and what the two parts of u leave out (4 * 2^-24 of it)
+        # every product and sum in binary32, in any order: k + rank terms, and what the two parts of u leave out (2^-20 of it, 16 * 2^-24)
         return y, HALF_STEP[self.dtype] * np.abs(y) + SMALLEST[self.dtype] + (2 * self.k + 2 * self.max_rank + 16) * 2.0 ** -24 * size
 
     def backward(self, x_held, positive, which):

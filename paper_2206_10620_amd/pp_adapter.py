@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from typing import NamedTuple, Optional, Union
 
 from .pp_block_gemm import BlockPlan, lib as _block_lib
@@ -45,6 +46,9 @@ def lib() -> C.CDLL:
 
 def pp_act8_bytes(rows: int, n: int) -> int:
     return lib().pp_act8_bytes(rows, n)
+
+
+_act8_bytes = functools.lru_cache(maxsize=1024)(pp_act8_bytes)
 
 
 def pp_act8_pack(x_dev: int, rows: int, n: int, dtype: int, held_dev: int, hip_stream: int = 0) -> int:
@@ -119,30 +123,35 @@ def _torch_dtype(dtype: int):
 
 class _Call:
     """The device and stream of a call: the tensors' device is made current, and what the call allocates belongs to the stream it
-    runs on.  On the current device and stream, the usual case, nothing has to be changed or put back."""
-
-    __slots__ = ("_device", "_stream", "_index")
+    runs on."""
 
     def __init__(self, device, stream: Optional[int]):
-        t = _TORCH or _torch()
-        self._index = device.index
-        self._device = None if device.index == t.cuda.current_device() else t.cuda.device(device)
+        t = _torch()
+        self._device = t.cuda.device(device)
         self._stream = None
         if stream is not None:
             self._stream = t.cuda.stream(t.cuda.ExternalStream(stream, device=device) if stream else t.cuda.default_stream(device))
 
     def __enter__(self) -> int:
-        if self._device is not None:
-            self._device.__enter__()
+        self._device.__enter__()
         if self._stream is not None:
             self._stream.__enter__()
-        return _TORCH.cuda.current_stream(self._index).cuda_stream
+        return _TORCH.cuda.current_stream().cuda_stream
 
     def __exit__(self, *exc):
         if self._stream is not None:
             self._stream.__exit__(*exc)
-        if self._device is not None:
-            self._device.__exit__(*exc)
+        self._device.__exit__(*exc)
+
+
+def _on(device, stream: Optional[int], call):
+    """call(handle of the stream it is to run on).  On the current device and stream, the usual case, nothing has to be changed and put
+    back: two contexts would take longer than a small kernel."""
+    t = _TORCH or _torch()
+    if stream is None and t.cuda.current_device() == device.index:
+        return call(t._C._cuda_getCurrentRawStream(device.index))
+    with _Call(device, stream) as s:
+        return call(s)
 
 
 def _check_status(st: int, what: str) -> None:
@@ -159,29 +168,36 @@ def _matrix(t, rows: int, n: Optional[int], dtype: int, device=None):
 class Act8:
     """A matrix [rows, n] held in 8 bits (buffer: pp_act8.h's form)."""
 
+    __slots__ = ("buffer", "rows", "n", "dtype")
+
     def __init__(self, buffer, rows: int, n: int, dtype: int):
         self.buffer, self.rows, self.n, self.dtype = buffer, rows, n, dtype
 
     def unpack(self, dtype: Optional[int] = None, stream: Optional[int] = None):
         """The values held, as a tensor of dtype (default: that of the tensor that was packed)."""
-        torch = _torch()
         dtype = self.dtype if dtype is None else dtype
-        with _Call(self.buffer.device, stream) as s:
-            out = torch.empty((self.rows, self.n), dtype=_torch_dtype(dtype), device=self.buffer.device)
-            _check_status(pp_act8_unpack(self.buffer.data_ptr(), self.rows, self.n, dtype, out.data_ptr(), s), "pp_act8_unpack")
-        return out
+        device = self.buffer.device
+
+        def call(s):
+            out = _TORCH.empty((self.rows, self.n), dtype=_torch_dtype(dtype), device=device)
+            _check_status(lib().pp_act8_unpack(self.buffer.data_ptr(), self.rows, self.n, dtype, out.data_ptr(), s), "pp_act8_unpack")
+            return out
+        return _on(device, stream, call)
 
 
 def act8_pack(x, stream: Optional[int] = None) -> Act8:
     """x [rows, n] (fp16 or fp32, on the GPU) in 8 bits."""
-    torch = _torch()
-    assert x.is_cuda and x.is_contiguous() and x.dim() == 2 and x.dtype in (torch.float16, torch.float32)
-    rows, n = x.shape
+    torch = _TORCH or _torch()
     dtype = PP_F16 if x.dtype == torch.float16 else PP_F32
-    with _Call(x.device, stream) as s:
-        buf = torch.empty(pp_act8_bytes(rows, n), dtype=torch.uint8, device=x.device)
-        _check_status(pp_act8_pack(x.data_ptr(), rows, n, dtype, buf.data_ptr(), s), "pp_act8_pack")
-    return Act8(buf, rows, n, dtype)
+    assert x.is_cuda and x.is_contiguous() and x.dim() == 2 and x.dtype == _torch_dtype(dtype)
+    rows, n = x.shape
+    device = x.device
+
+    def call(s):
+        buf = torch.empty(_act8_bytes(rows, n), dtype=torch.uint8, device=device)
+        _check_status(lib().pp_act8_pack(x.data_ptr(), rows, n, dtype, buf.data_ptr(), s), "pp_act8_pack")
+        return Act8(buf, rows, n, dtype)
+    return _on(device, stream, call)
 
 
 class InputGradient(NamedTuple):
@@ -204,80 +220,79 @@ class AdapterBank:
         with torch.cuda.device(self.device):
             st, self.handle = pp_adapter_plan(m, k, slots, max_rank, dtype)
         _check_status(st, "pp_adapter_plan")
-        self._sizes = {}                                # n -> bytes of u and v
-
-    def _state_bytes(self, n: int):
-        """Bytes of u and of v for n tokens (0: the call that follows refuses n)."""
-        sizes = self._sizes.get(n)
-        if sizes is None:
-            sizes = self._sizes[n] = (pp_adapter_u_bytes(self.handle, n), pp_adapter_v_bytes(self.handle, n))
-        return sizes
+        self._state_bytes = functools.lru_cache(maxsize=1024)(lambda n, h=self.handle: (pp_adapter_u_bytes(h, n), pp_adapter_v_bytes(h, n)))
+        self._work_bytes = functools.lru_cache(maxsize=1024)(lambda n, count, h=self.handle: pp_adapter_work_bytes(h, n, count))
 
     def _slots_of(self, slot_of, n: int):
         torch = _torch()
         assert slot_of.is_cuda and slot_of.is_contiguous() and slot_of.dtype == torch.int32 and tuple(slot_of.shape) == (n,) and slot_of.device == self.device
 
     def _opaque(self, nbytes: int):
-        torch = _torch()
-        return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        return _TORCH.empty(nbytes, dtype=_TORCH.uint8, device=self.device)
 
     def load(self, slot: int, a, b, scale: float, stream: Optional[int] = None) -> None:
         """a [rank, k] and b [m, rank] into a slot.  They may be freed or changed once the stream has got there."""
         rank = a.shape[0]
         _matrix(a, rank, self.k, self.dtype, self.device)
         _matrix(b, self.m, rank, self.dtype, self.device)
-        with _Call(self.device, stream) as s:
-            _check_status(pp_adapter_load(self.handle, slot, rank, scale, a.data_ptr(), b.data_ptr(), s), "pp_adapter_load")
+        _on(self.device, stream, lambda s: _check_status(
+            lib().pp_adapter_load(self.handle, slot, rank, scale, a.data_ptr(), b.data_ptr(), s), "pp_adapter_load"))
 
     def unload(self, slot: int, stream: Optional[int] = None) -> None:
-        with _Call(self.device, stream) as s:
-            _check_status(pp_adapter_load(self.handle, slot, 0, 0.0, None, None, s), "pp_adapter_load")
+        _on(self.device, stream, lambda s: _check_status(lib().pp_adapter_load(self.handle, slot, 0, 0.0, None, None, s), "pp_adapter_load"))
 
     def project(self, x, slot_of, stream: Optional[int] = None):
         """u = A x alone (opaque, for grad_weights): what run(keep=True) returns beside y."""
         _matrix(x, self.k, None, self.dtype, self.device)
         n = x.shape[1]
         self._slots_of(slot_of, n)
-        with _Call(self.device, stream) as s:
+
+        def call(s):
             u = self._opaque(self._state_bytes(n)[0])
-            _check_status(pp_adapter_project(self.handle, x.data_ptr(), slot_of.data_ptr(), u.data_ptr(), n, s), "pp_adapter_project")
-        return u
+            _check_status(lib().pp_adapter_project(self.handle, x.data_ptr(), slot_of.data_ptr(), u.data_ptr(), n, s), "pp_adapter_project")
+            return u
+        return _on(self.device, stream, call)
 
     def run(self, plan: BlockPlan, x, slot_of, y=None, keep: bool = False, stream: Optional[int] = None):
         """y = act(W x + bias + c B (A x)); with keep also u, which grad_weights takes."""
-        torch = _torch()
         _matrix(x, self.k, None, self.dtype, self.device)
         n = x.shape[1]
         self._slots_of(slot_of, n)
-        with _Call(self.device, stream) as s:
-            if y is None:
-                y = torch.empty((self.m, n), dtype=x.dtype, device=self.device)
+        if y is not None:
             _matrix(y, self.m, n, self.dtype, self.device)
+
+        def call(s):
+            out = _TORCH.empty((self.m, n), dtype=x.dtype, device=self.device) if y is None else y
             u = self._opaque(self._state_bytes(n)[0])
-            _check_status(pp_adapter_run(self.handle, plan.handle, x.data_ptr(), slot_of.data_ptr(), u.data_ptr(), y.data_ptr(), n, s), "pp_adapter_run")
-        return (y, u) if keep else y
+            _check_status(lib().pp_adapter_run(self.handle, plan.handle, x.data_ptr(), slot_of.data_ptr(), u.data_ptr(), out.data_ptr(), n, s),
+                          "pp_adapter_run")
+            return (out, u) if keep else out
+        return _on(self.device, stream, call)
 
     def grad_input(self, plan_t: Optional[BlockPlan], dy, slot_of, gate: Optional[Act8] = None, stream: Optional[int] = None) -> InputGradient:
         """dx = W^T g + c A^T (B^T g) through plan_t, the plan of the transposed weights (None: no dx), g = dy where the output held
         in gate is above 0 (None: everywhere)."""
-        torch = _torch()
         _matrix(dy, self.m, None, self.dtype, self.device)
         n = dy.shape[1]
         self._slots_of(slot_of, n)
         assert gate is None or (gate.rows == self.m and gate.n == n and gate.buffer.device == self.device)
-        with _Call(self.device, stream) as s:
+
+        def call(s):
+            torch = _TORCH
             g = dy if gate is None else torch.empty_like(dy)
             dx = None if plan_t is None else torch.empty((self.k, n), dtype=dy.dtype, device=self.device)
             v = self._opaque(self._state_bytes(n)[1])
-            st = pp_adapter_grad_input(self.handle, None if plan_t is None else plan_t.handle, dy.data_ptr(), None if gate is None else gate.buffer.data_ptr(),
-                                       None if gate is None else g.data_ptr(), slot_of.data_ptr(), v.data_ptr(), None if dx is None else dx.data_ptr(), n, s)
+            st = lib().pp_adapter_grad_input(self.handle, None if plan_t is None else plan_t.handle, dy.data_ptr(),
+                                             None if gate is None else gate.buffer.data_ptr(), None if gate is None else g.data_ptr(),
+                                             slot_of.data_ptr(), v.data_ptr(), None if dx is None else dx.data_ptr(), n, s)
             _check_status(st, "pp_adapter_grad_input")
-        return InputGradient(dx, v, g)
+            return InputGradient(dx, v, g)
+        return _on(self.device, stream, call)
 
     def grad_weights(self, x: Union["Act8", object], u, g, v, slot_of, which, stream: Optional[int] = None):
         """Gradients of the slots that which (int32 tensor) lists: da [count, max_rank, k], db [count, m, max_rank], fp32.  x: the
         layer's input, as it was or in 8 bits; u of run or project, g and v of grad_input."""
-        torch = _torch()
+        torch = _TORCH or _torch()
         _matrix(g, self.m, None, self.dtype, self.device)
         n = g.shape[1]
         self._slots_of(slot_of, n)
@@ -289,19 +304,23 @@ class AdapterBank:
         assert which.is_cuda and which.is_contiguous() and which.dtype == torch.int32 and which.dim() == 1 and which.device == self.device
         assert (u.numel(), v.numel()) == self._state_bytes(n)
         count = which.shape[0]
-        with _Call(self.device, stream) as s:
+
+        def call(s):
             da = torch.empty((count, self.max_rank, self.k), dtype=torch.float32, device=self.device)
             db = torch.empty((count, self.m, self.max_rank), dtype=torch.float32, device=self.device)
-            work = self._opaque(pp_adapter_work_bytes(self.handle, n, count))
-            st = pp_adapter_grad_weights(self.handle, (x.buffer if held else x).data_ptr(), 1 if held else 0, u.data_ptr(), g.data_ptr(), v.data_ptr(),
-                                         slot_of.data_ptr(), which.data_ptr(), count, da.data_ptr(), db.data_ptr(), work.data_ptr(), n, s)
+            work = self._opaque(self._work_bytes(n, count))
+            st = lib().pp_adapter_grad_weights(self.handle, (x.buffer if held else x).data_ptr(), 1 if held else 0, u.data_ptr(), g.data_ptr(),
+                                               v.data_ptr(), slot_of.data_ptr(), which.data_ptr(), count, da.data_ptr(), db.data_ptr(),
+                                               work.data_ptr(), n, s)
             _check_status(st, "pp_adapter_grad_weights")
-        return da, db
+            return da, db
+        return _on(self.device, stream, call)
 
     def close(self):
         if self.handle is not None:
             pp_adapter_destroy(self.handle)
             self.handle = None
+            self._state_bytes, self._work_bytes = lambda n: (0, 0), lambda n, count: 0      # calls from now on are refused
 
     def __del__(self):
         try:

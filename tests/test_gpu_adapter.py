@@ -410,3 +410,10 @@ def test_refusals_that_need_a_device():
         s.bank.run(s.plan, s.x.t(), s.slot_of)
     with pytest.raises(AssertionError):
         s.bank.run(s.plan, s.x, s.slot_of.long())
+    s.bank.close()
+    s.bank.close()
+    for call in (lambda: s.bank.run(s.plan, s.x, s.slot_of), lambda: s.bank.project(s.x, s.slot_of), lambda: s.bank.unload(0),
+                 lambda: s.bank.grad_input(s.plan_t, s.dy, s.slot_of)):
+        with pytest.raises(pp.PPError) as e:
+            call()
+        assert e.value.status == pp.PP_ERR_NULL

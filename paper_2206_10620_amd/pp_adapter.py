@@ -165,12 +165,19 @@ def _matrix(t, rows: int, n: Optional[int], dtype: int, device=None):
     assert device is None or t.device == device
 
 
+def _opaque_ok(t, device):
+    """t is memory of the kind that the calls here leave their state in."""
+    assert t.is_cuda and t.device == device and t.element_size() == 1 and t.is_contiguous()
+
+
 class Act8:
     """A matrix [rows, n] held in 8 bits (buffer: pp_act8.h's form)."""
 
     __slots__ = ("buffer", "rows", "n", "dtype")
 
     def __init__(self, buffer, rows: int, n: int, dtype: int):
+        assert 0 < _act8_bytes(rows, n) == buffer.numel()
+        _opaque_ok(buffer, buffer.device)
         self.buffer, self.rows, self.n, self.dtype = buffer, rows, n, dtype
 
     def unpack(self, dtype: Optional[int] = None, stream: Optional[int] = None):
@@ -303,6 +310,8 @@ class AdapterBank:
             _matrix(x, self.k, n, self.dtype, self.device)
         assert which.is_cuda and which.is_contiguous() and which.dtype == torch.int32 and which.dim() == 1 and which.device == self.device
         assert (u.numel(), v.numel()) == self._state_bytes(n)
+        _opaque_ok(u, self.device)
+        _opaque_ok(v, self.device)
         count = which.shape[0]
 
         def call(s):

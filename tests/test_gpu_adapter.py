@@ -417,3 +417,20 @@ def test_refusals_that_need_a_device():
         with pytest.raises(pp.PPError) as e:
             call()
         assert e.value.status == pp.PP_ERR_NULL
+
+
+def test_states_of_another_kind_are_refused():
+    p = Problem("f16", 64, 80, 40, [8], 8, "one", seed=17)
+    s = Setup(p)
+    _, u = s.bank.run(s.plan, s.x, s.slot_of, keep=True)
+    g = s.bank.grad_input(s.plan_t, s.dy, s.slot_of)
+    which = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for bad_u, bad_v in ((u.cpu(), g.v), (u, g.v.cpu()), (u[1:], g.v), (u, g.v[:-1]), (torch.zeros(u.numel(), device="cuda"), g.v)):
+        with pytest.raises(AssertionError):
+            s.bank.grad_weights(s.x, bad_u, g.g, bad_v, s.slot_of, which)
+    held = pp.act8_pack(s.x)
+    for buffer, rows, n in ((held.buffer.cpu(), 80, 40), (held.buffer, 80, 129), (held.buffer[1:], 80, 40), (held.buffer, 0, 40), (s.x, 80, 40)):
+        with pytest.raises(AssertionError):
+            pp.Act8(buffer, rows, n, pp.PP_F16)
+    da, db = s.bank.grad_weights(pp.Act8(held.buffer, 80, 40, pp.PP_F16), u, g.g, g.v, s.slot_of, which)
+    assert da.shape == (1, 8, 80) and db.shape == (1, 64, 8)

@@ -58,7 +58,7 @@ template <typename T, int FT, int RG, bool GATED> void project_as(const K8Projec
     hipLaunchKernelGGL((k8_project<T, FT, RG, GATED>), grid, dim3(64 * kProjectWaves), 0, stream, a);
 }
 template <typename T, int FT, bool GATED> void project_rg(const K8Project& a, dim3 grid, hipStream_t stream) {
-    constexpr int most = (sizeof(T) == 4 && FT == 4) || FT == 8 ? 2 : 4;      // rank tiles in registers at a time: four would spill there
+    constexpr int most = sizeof(T) == 4 && FT == 4 ? 2 : 4;      // rank tiles in registers at a time: four would spill there
     if (a.rank_pad <= 16) project_as<T, FT, 1, GATED>(a, grid, stream);
     else if (a.rank_pad <= 32) project_as<T, FT, 2, GATED>(a, grid, stream);
     else project_as<T, FT, most, GATED>(a, grid, stream);
@@ -66,8 +66,7 @@ template <typename T, int FT, bool GATED> void project_rg(const K8Project& a, di
 template <typename T, bool GATED> void project_ft(int ft, const K8Project& a, dim3 grid, hipStream_t stream) {
     if (ft == 1) project_rg<T, 1, GATED>(a, grid, stream);
     else if (ft == 2) project_rg<T, 2, GATED>(a, grid, stream);
-    else if (ft == 4) project_rg<T, 4, GATED>(a, grid, stream);
-    else if constexpr (GATED && sizeof(T) == 2) project_rg<T, 8, GATED>(a, grid, stream);
+    else project_rg<T, 4, GATED>(a, grid, stream);
 }
 
 // where the sums of what a projection left start
@@ -78,21 +77,20 @@ const float* sums_of(const void* state, int n) { return reinterpret_cast<const f
 void launch_project(const pp_adapter_bank_t* b, bool of_a, const void* x, const void* gate, void* g, const int32_t* slot_of, void* u, int n, hipStream_t stream) {
     K8Project a{};
     a.rows = of_a ? b->k : b->m;
-    const ProjectShape sh = project_shape(a.rows, n, !of_a);
+    const ProjectShape sh = project_shape(a.rows, n, b->dtype == PP_F16, !of_a);
     a.x = x, a.gate = static_cast<const int8_t*>(gate), a.g = g, a.slot_of = slot_of, a.rank = b->rank, a.scale = b->scale;
     a.tokens = static_cast<KxToken*>(u), a.u = sums_of(u, n);
     a.operands = of_a ? b->a_project : b->b_project;
     a.slot_elems = (of_a ? b->a_project_slot : b->b_project_slot) / elem(b);
     a.gate_pitch = act8_pitch(n);
     a.n = n, a.steps = (a.rows + 31) / 32, a.slots = b->slots, a.rank_pad = b->rank_pad, a.splits = sh.splits;
-    const int ft = project_tokens(sh, gate != nullptr, b->dtype == PP_F16, b->rank_pad), tiles = (n + 16 * ft - 1) / (16 * ft);
-    const dim3 grid((unsigned)(tiles * sh.splits), (unsigned)project_subsets(tiles, sh.splits, ft, b->slots));
+    const dim3 grid((unsigned)(sh.tiles * sh.splits), (unsigned)project_subsets(sh, b->slots));
     if (b->dtype == PP_F16) {
-        if (gate) project_ft<_Float16, true>(ft, a, grid, stream);
-        else project_ft<_Float16, false>(ft, a, grid, stream);
+        if (gate) project_ft<_Float16, true>(sh.ft, a, grid, stream);
+        else project_ft<_Float16, false>(sh.ft, a, grid, stream);
     } else {
-        if (gate) project_ft<float, true>(ft, a, grid, stream);
-        else project_ft<float, false>(ft, a, grid, stream);
+        if (gate) project_ft<float, true>(sh.ft, a, grid, stream);
+        else project_ft<float, false>(sh.ft, a, grid, stream);
     }
 }
 
@@ -100,7 +98,7 @@ void launch_project(const pp_adapter_bank_t* b, bool of_a, const void* x, const 
 pp_status_t launch_product(const pp_adapter_bank_t* b, bool of_b, const pp_block_gemm_plan_t* plan, const void* x, const void* u, void* y, int n,
                            hipStream_t stream) {
     const int rows_in = of_b ? b->k : b->m;
-    const int splits = project_shape(rows_in, n, !of_b).splits;
+    const int splits = project_shape(rows_in, n, b->dtype == PP_F16, !of_b).splits;
     const int64_t split_elems = kx_share(n, b->rank_pad);
     if (b->dtype == PP_F16) {
         K4Expand e{};
@@ -205,8 +203,8 @@ pp_status_t pp_adapter_load(pp_adapter_bank_t* bank, int32_t slot, int32_t rank,
     return launched();
 }
 
-int64_t pp_adapter_u_bytes(const pp_adapter_bank_t* bank, int32_t n) { return bank && tokens_ok(bank, n) ? adapter_state_bytes(bank->k, n, bank->rank_pad, false) : 0; }
-int64_t pp_adapter_v_bytes(const pp_adapter_bank_t* bank, int32_t n) { return bank && tokens_ok(bank, n) ? adapter_state_bytes(bank->m, n, bank->rank_pad, true) : 0; }
+int64_t pp_adapter_u_bytes(const pp_adapter_bank_t* bank, int32_t n) { return bank && tokens_ok(bank, n) ? adapter_state_bytes(bank->k, n, bank->rank_pad, bank->dtype == PP_F16, false) : 0; }
+int64_t pp_adapter_v_bytes(const pp_adapter_bank_t* bank, int32_t n) { return bank && tokens_ok(bank, n) ? adapter_state_bytes(bank->m, n, bank->rank_pad, bank->dtype == PP_F16, true) : 0; }
 int64_t pp_adapter_work_bytes(const pp_adapter_bank_t* bank, int32_t n, int32_t count) {
     return bank && tokens_ok(bank, n) && count >= 1 && count <= 65535 ? grad_work(bank->m, bank->k, n, count, bank->rank_pad, bank->dtype == PP_F16).bytes : 0;
 }
@@ -310,7 +308,7 @@ pp_status_t pp_adapter_grad_weights(const pp_adapter_bank_t* bank, const void* x
     K8Turn t{};
     t.out = turned;
     t.w[0] = sums_of(v_dev, n), t.w[1] = sums_of(u_dev, n);
-    t.splits[0] = project_shape(bank->m, n, true).splits, t.splits[1] = project_shape(bank->k, n, false).splits;
+    t.splits[0] = project_shape(bank->m, n, half, true).splits, t.splits[1] = project_shape(bank->k, n, half, false).splits;
     t.slot_of = slot_of_dev, t.which = which_dev, t.rank = bank->rank, t.scale = bank->scale;
     t.n = n, t.slots = bank->slots, t.blocks = (n + kAct8Block - 1) / kAct8Block, t.rank_pad = bank->rank_pad, t.x_is_act8 = x_is_act8 ? 1 : 0;
     const dim3 turns((unsigned)t.blocks, (unsigned)count, (unsigned)(2 * (bank->rank_pad / 16)));

@@ -29,43 +29,40 @@ inline int64_t adapter_expand_elems(int width, int rank_pad, bool half) {
 // A projection (u = A x, or v = B^T g): a workgroup takes 16 ft tokens and one of `splits` shares of the rows, whose sums are kept apart and
 // added by whoever reads them, and every `subsets`-th of the slots that its tokens name.  Splits follow from the sizes alone, since they
 // are part of the layout of what is left.
-//   ft: with one token to a lane a row gives 32 bytes, and many tokens ask the cache for every line four times; few tokens make few
-//   workgroups.  4096 rows, rank 16, 4 / 2 / 1 tokens to a lane: 4096 tokens 8.6 / 10.9 / 19.8 us, 2048 7.2 / 7.0 / 8.3, 1024
-//   7.2 / 5.9 / 5.6, 64 - / - / 5.2.  Where the gate is read and g written too, and there are three streams, twice as many: in binary16 4096
-//   tokens 22.9 us with 8, 25.6 with 4, 2000 tokens of rank 64 36 with 4, 46.8 with 2.
-//   splits: more shares fill the GPU, but the product that reads u does so once for every 64 rows of its own: 4096 x 4096 on 4096
-//   tokens, projection and product less the product without adapters: 2 shares 11.1 us, 4 11.1, 8 15.2 with rank 16, 19.9 and 26.1 with
-//   rank 32; 512 tokens 13.2 and 12.2.  v's projection may also read the gate and write g: 2 shares 97 us for all of a backward pass's
-//   first half, 4 90.6.
+//   ft: with one token of binary16 to a lane a row gives 32 bytes, and many tokens ask the cache for every line four times; few tokens make
+//   few workgroups.  4096 rows, rank 16, 4 / 2 / 1 tokens to a lane: 4096 tokens 9.4 / 13.9 / - us, 2048 8.3 / 8.0 / 13.5, 1024
+//   8.2 / 5.4 / 7.5, 512 8.2 / 5.3 / 4.8.  A value of binary32 is twice as wide: 2048 rows, rank 32, 4096 tokens 18.7 / 11.1 / -, 1024
+//   18.3 / 10.1 / 7.5.  More than one to a lane only where there are more tokens than a tile has: k8_project relies on that.
+//   splits: more shares fill the GPU, but the product that reads u does so once for every 64 rows of its own.  4096 x 4096, projection and
+//   product less the product without adapters, 2 / 4 / 8 shares: 512 tokens of eight slots of rank 32 12.7 / 10.8 / 15.0 us, 1024 of 64
+//   slots of rank 16 15.6 / 18.1 / 24.9.  v's projection may also read the gate and write g; a backward pass's whole first half: 1024
+//   tokens of rank 16 49.9 / 46.2 / 48.2, 4096 85.2 / 85.2 / 92.3, of rank 64 101.6 / 116.5 / 136.2.
 constexpr int kProjectWaves = 8;
 struct ProjectShape {
     int ft, tiles, splits;
 };
-inline ProjectShape project_shape(int rows, int n, bool of_v) {
+inline ProjectShape project_shape(int rows, int n, bool half, bool of_v) {
     ProjectShape s;
-    s.ft = n <= 1024 ? 1 : (n <= 2048 ? 2 : 4);
+    const int unit = half ? 512 : 1024;
+    s.ft = n <= unit ? 1 : (n <= 4 * unit ? 2 : 4);
     s.tiles = (n + 16 * s.ft - 1) / (16 * s.ft);
     s.splits = 512 / s.tiles;
-    const int steps = (rows + 31) / 32, most = (steps + 2 * kProjectWaves - 1) / (2 * kProjectWaves), limit = of_v || n <= 512 ? 4 : 2;
+    const int steps = (rows + 31) / 32, most = (steps + 2 * kProjectWaves - 1) / (2 * kProjectWaves), limit = n <= (of_v ? 1024 : 512) ? 4 : 2;
     if (s.splits > most) s.splits = most;
     if (s.splits > limit) s.splits = limit;
     if (s.splits < 1) s.splits = 1;
     return s;
 }
-inline int project_tokens(const ProjectShape& s, bool gated, bool half, int rank_pad) {      // to a lane, as launched
-    if (!gated || !half || s.ft == 1) return s.ft;
-    return rank_pad > 32 ? 4 : 2 * s.ft;                    // eight tokens and four rank tiles would not fit the registers
-}
-// 64 tokens with a slot of rank 16 each: 10.0 us with one subset, 7.2 with 16.
-inline int project_subsets(int tiles, int splits, int ft, int slots) {
-    int z = 512 / (tiles * splits);
-    const int most = slots < 16 * ft ? slots : 16 * ft;
+// 64 tokens with a slot of rank 16 each: 26.1 us with one subset, 9.3 with 4, 5.9 with 16.
+inline int project_subsets(const ProjectShape& s, int slots) {
+    int z = 512 / (s.tiles * s.splits);
+    const int most = slots < 16 * s.ft ? slots : 16 * s.ft;
     if (z > most) z = most;
     return z < 1 ? 1 : z;
 }
 // What a projection leaves: 16 bytes for each token, then the sums, of whole groups of 32 tokens.
-inline int64_t adapter_state_bytes(int rows, int n, int rank_pad, bool of_v) {
-    return (int64_t)n * 16 + (int64_t)project_shape(rows, n, of_v).splits * (((int64_t)n + 31) / 32 * 32) * rank_pad * 4;
+inline int64_t adapter_state_bytes(int rows, int n, int rank_pad, bool half, bool of_v) {
+    return (int64_t)n * 16 + (int64_t)project_shape(rows, n, half, of_v).splits * (((int64_t)n + 31) / 32 * 32) * rank_pad * 4;
 }
 
 // The gradients of A (k rows of x) and B (m rows of g): a workgroup takes 64 rw rows of one of them and one of `splits` shares of the

@@ -127,48 +127,58 @@ __global__ __launch_bounds__(64 * kProjectWaves) void k8_project(const K8Project
     const int lane = (int)(threadIdx.x & 63u), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int c = lane & 15, g = lane >> 4;
     const int tile = (int)blockIdx.x / a.splits, split = (int)blockIdx.x - tile * a.splits;
-    const int t0 = tile * 16 * FT, mine0 = t0 + c * FT;
+    // The last tile is moved back to end with the last token, or, of one token to a lane, its last lanes repeat that: every load is whole
+    const int own0 = tile * 16 * FT, t0 = FT == 1 ? own0 : min(own0, a.n - 16 * FT);
+    const int mine0 = FT == 1 ? min(own0 + c, a.n - 1) : t0 + c * FT;
     const int s0 = (int)((int64_t)a.steps * split / a.splits), s1 = (int)((int64_t)a.steps * (split + 1) / a.splits);
     const int w0 = s0 + (int)((int64_t)(s1 - s0) * wave / W), w1 = s0 + (int)((int64_t)(s1 - s0) * (wave + 1) / W);
-    const int left = a.n - mine0;
     const T* x = static_cast<const T*>(a.x);
     float* u = a.u + split * kx_share(a.n, a.rank_pad);
 
     typedef k8_any<T, FT> Piece;
-    // Rows of a step.  WHOLE: all are there, and all tokens of the tile; no branch stands between the loads then, which would make
-    // the wait for one a wait for all.
-    auto load = [&](auto whole, auto write_g, int st, Piece (&v)[8]) {
+    typedef k8_any<int8_t, FT> Gate;
+    struct Rows {
+        Piece v[8];
+        Gate q[GATED ? 8 : 1];
+        k8_v8<T> op[RG];
+    };
+    // Steps on their way at a time, as registers allow: one step's loads are back in about 1 us, and few wavefronts have more than eight
+    constexpr int kStage = (FT * (int)sizeof(T) < 4 ? 8 : FT * (int)sizeof(T) * 2) + (GATED ? 8 : 0) + RG * (int)sizeof(T) * 2;
+    constexpr int kAhead = kStage <= (GATED ? 24 : 40) ? 4 : 2;
+    // Where row i of a lane's eight of a step is: what is the same for all lanes, and 32 bits.  WHOLE: all rows are there; otherwise the
+    // last one is read in place of those behind it, and 0 taken: no branch between the loads, which would make the wait for one a wait for all.
+    auto spot = [&](auto whole, const auto* p, int64_t pitch, int st, int i) {
         constexpr bool WHOLE = decltype(whole)::value;
-        const int row0 = st * 32 + g * 8;
-        const T* src = x + (int64_t)row0 * a.n + mine0;
+        const int row = WHOLE ? g * 8 : min(g * 8 + i, a.rows - 1 - st * 32);
+        const char* all = reinterpret_cast<const char*>(p + (int64_t)(st * 32 + (WHOLE ? i : 0)) * pitch);
+        return all + (uint32_t)(row * (int)pitch + mine0) * (uint32_t)sizeof(*p);
+    };
+    auto load = [&](auto whole, int st, Rows& r) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.v[i] = *reinterpret_cast<const Piece*>(spot(whole, x, a.n, st, i));
+        if constexpr (GATED) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r.q[i] = *reinterpret_cast<const Gate*>(spot(whole, a.gate, a.gate_pitch, st, i));
+        }
+    };
+    // What was loaded, behind the gate
+    auto take = [&](auto whole, auto write_g, int st, Rows& r) {
+        constexpr bool WHOLE = decltype(whole)::value;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if constexpr (WHOLE) v[i] = *reinterpret_cast<const Piece*>(src + (int64_t)i * a.n);
-            else v[i] = k8_load<T, FT>(src + (int64_t)i * a.n, row0 + i < a.rows ? left : 0);
-        }
-        if constexpr (GATED) {
-            typedef k8_any<int8_t, FT> Gate;
-            Gate q[8];
-            const int8_t* gate = a.gate + (int64_t)row0 * a.gate_pitch + mine0;
+            const bool there = WHOLE || st * 32 + g * 8 + i < a.rows;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if constexpr (WHOLE) q[i] = *reinterpret_cast<const Gate*>(gate + i * a.gate_pitch);
-                else q[i] = k8_load<int8_t, FT>(gate + i * a.gate_pitch, row0 + i < a.rows && left > 0 ? FT : 0);
+            for (int f = 0; f < FT; ++f) {
+                bool through = there;
+                if constexpr (GATED) through = through && k8_at<Gate, int8_t>(r.q[i], f) > 0;
+                if (!through) k8_put(r.v[i], f, (T)0.0f);
             }
-            T* dst = static_cast<T*>(a.g) + (int64_t)row0 * a.n + mine0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-#pragma unroll
-                for (int f = 0; f < FT; ++f)
-                    if (!(k8_at<Gate, int8_t>(q[i], f) > 0)) k8_put(v[i], f, (T)0.0f);
-                if constexpr (decltype(write_g)::value) {
-                    if constexpr (WHOLE) *reinterpret_cast<Piece*>(dst + (int64_t)i * a.n) = v[i];
-                    else if (row0 + i < a.rows) k8_store<T, FT>(dst + (int64_t)i * a.n, left, v[i]);
-                }
+            if constexpr (decltype(write_g)::value) {
+                if (there) *reinterpret_cast<Piece*>(const_cast<char*>(spot(whole, static_cast<const T*>(a.g), a.n, st, i))) = r.v[i];
             }
         }
     };
-    const bool whole_here = t0 + 16 * FT <= a.n && w1 * 32 <= a.rows;
+    const int full = min(w1, a.rows / 32);                       // steps from here on lack rows: the last one at most
 
     // One slot's tokens (slot -1: only the gate), ranks from tile rt0 on.
     auto pass = [&](int slot, int rt0, int tiles, bool is_first) {
@@ -178,48 +188,56 @@ __global__ __launch_bounds__(64 * kProjectWaves) void k8_project(const K8Project
 #pragma unroll
             for (int f = 0; f < FT; ++f) acc[r][f] = k8_f4(0.0f);
         const T* ops = static_cast<const T*>(a.operands) + (slot < 0 ? 0 : slot * a.slot_elems) + (int64_t)rt0 * a.steps * 512 + lane * 8;
-        // the next step's rows are on their way while this one's are multiplied
-        auto steps = [&](auto whole, auto write_g) {
-            Piece v[8], next[8];
-            k8_v8<T> op[RG];
-            auto load_ops = [&](int st) {
+        // The operands come with the rows: loads are waited for in their order
+        auto steps = [&](auto whole, auto write_g, int from, int to) {
+            asm("" : "+s"(from));                                // addresses are not kept from one pass for the next: registers
+            auto fetch = [&](int st, Rows& r) {
 #pragma unroll
-                for (int r = 0; r < RG; ++r)
-                    op[r] = *reinterpret_cast<const k8_v8<T>*>(ops + ((int64_t)(r < tiles ? r : 0) * a.steps + st) * 512);
+                for (int i = 0; i < RG; ++i) r.op[i] = *reinterpret_cast<const k8_v8<T>*>(ops + ((int64_t)(i < tiles ? i : 0) * a.steps + st) * 512);
+                load(whole, st, r);
+                __builtin_amdgcn_sched_barrier(0);
             };
-            auto multiply = [&]() {
+            auto multiply = [&](int st, Rows& r) {
+                take(whole, write_g, st, r);
 #pragma unroll
                 for (int f = 0; f < FT; ++f) {
                     k8_v8<T> b;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) b[i] = k8_at<Piece, T>(v[i], f);
+                    for (int i = 0; i < 8; ++i) b[i] = k8_at<Piece, T>(r.v[i], f);
 #pragma unroll
-                    for (int r = 0; r < RG; ++r)
-                        if (r < tiles) acc[r][f] = k8_mfma(op[r], b, acc[r][f]);
+                    for (int i = 0; i < RG; ++i)
+                        if (i < tiles) acc[i][f] = k8_mfma(r.op[i], b, acc[i][f]);
                 }
+                __builtin_amdgcn_sched_barrier(0);
             };
-            load(whole, write_g, w0, v);
-            for (int st = w0; st + 1 < w1; ++st) {
-                load_ops(st);
-                load(whole, write_g, st + 1, next);
-                multiply();
+            constexpr int P = decltype(whole)::value ? kAhead : 1;      // (the step that lacks rows is one)
+            Rows r[P];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = next[i];
+            for (int j = 0; j < P; ++j) fetch(min(from + j, to - 1), r[j]);
+            int st = from;
+            for (; st + 2 * P <= to; st += P) {
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    multiply(st + j, r[j]);
+                    fetch(st + P + j, r[j]);
+                }
             }
-            load_ops(w1 - 1);
-            multiply();
+#pragma unroll
+            for (int j = 0; j < P; ++j)
+                if (st + j < to) {
+                    multiply(st + j, r[j]);
+                    if (st + P + j < to) fetch(st + P + j, r[j]);
+                }
+#pragma unroll
+            for (int j = 0; j + 1 < P; ++j)
+                if (st + P + j < to) multiply(st + P + j, r[j]);
         };
-        if (w0 < w1) {
-            const std::true_type yes;
-            const std::false_type no;
-            if (GATED && is_first && blockIdx.y == 0) {
-                if (whole_here) steps(yes, std::integral_constant<bool, GATED>{});
-                else steps(no, std::integral_constant<bool, GATED>{});
-            } else {
-                if (whole_here) steps(yes, no);
-                else steps(no, no);
-            }
-        }
+        auto all = [&](auto write_g) {
+            if (w0 < full) steps(std::true_type{}, write_g, w0, full);
+            if (max(w0, full) < w1) steps(std::false_type{}, write_g, max(w0, full), w1);
+        };
+        if (GATED && is_first && blockIdx.y == 0) all(std::integral_constant<bool, GATED>{});
+        else all(std::false_type{});
         if (slot < 0) return;
         const int rank = a.rank[slot];
 #pragma unroll
@@ -236,7 +254,7 @@ __global__ __launch_bounds__(64 * kProjectWaves) void k8_project(const K8Project
                     for (int w = 1; w < W; ++w) v += red[w * FT * 64 + i];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) v[e] = j + e < rank ? v[e] : 0.0f;
-                    if (t < a.n && a.slot_of[t] == slot) *reinterpret_cast<k8_f4*>(u + kx_at(t, j, a.rank_pad)) = v;
+                    if (t >= own0 && t < a.n && a.slot_of[t] == slot) *reinterpret_cast<k8_f4*>(u + kx_at(t, j, a.rank_pad)) = v;
                 }
             }
         }
@@ -248,7 +266,7 @@ __global__ __launch_bounds__(64 * kProjectWaves) void k8_project(const K8Project
     for (int f = 0; f < FT; ++f) {
         const KxToken tok = kx_token(a.slot_of, a.rank, a.scale, a.slots, mine0 + f, a.n);
         sl[f] = tok.slot;
-        if (split == 0 && blockIdx.y == 0 && threadIdx.x < 16 && mine0 + f < a.n) a.tokens[mine0 + f] = tok;
+        if (split == 0 && blockIdx.y == 0 && threadIdx.x < 16) a.tokens[mine0 + f] = tok;
     }
     bool is_first = true;
     uint32_t leaders = 0;                                        // one token to a lane: the slots' first ones, from this workgroup's first on

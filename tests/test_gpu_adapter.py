@@ -434,3 +434,16 @@ def test_states_of_another_kind_are_refused():
             pp.Act8(buffer, rows, n, pp.PP_F16)
     da, db = s.bank.grad_weights(pp.Act8(held.buffer, 80, 40, pp.PP_F16), u, g.g, g.v, s.slot_of, which)
     assert da.shape == (1, 8, 80) and db.shape == (1, 64, 8)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("shape", [(130, 300, 513, [16, 3], 16, "runs"), (1056, 640, 545, [40, 64], 64, "mixed"), (96, 33, 1025, [20], 32, "one"),
+                                   (544, 577, 2049, [16, 9, 12], 16, "runs"), (300, 129, 4097, [64, 33], 64, "runs"), (97, 256, 4223, [30, 0], 32, "values")],
+                         ids=lambda s: "x".join(str(v) for v in s[:3]))
+def test_tiles_of_several_tokens_to_a_lane(shape, dtype):
+    """Token counts that end inside a tile, row counts that end inside a step, wavefronts with few and with many steps."""
+    m, k, n, ranks, max_rank, order = shape
+    for relu in (False, True):
+        s = Setup(Problem(dtype, m, k, n, ranks, max_rank, order, relu=relu, seed=18))
+        s.check_forward()
+        s.check_backward(held=relu, relu=relu)

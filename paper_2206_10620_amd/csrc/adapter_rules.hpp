@@ -66,9 +66,9 @@ inline int64_t adapter_state_bytes(int rows, int n, int rank_pad, bool half, boo
 }
 
 // The gradients of A (k rows of x) and B (m rows of g): a workgroup takes 64 rw rows of one of them and one of `splits` shares of the
-// blocks of 128 tokens.  Shares fill the GPU but cost a launch that joins them, 4 us.  4096 + 4096 rows, 4096 tokens, one slot: 1 share
-// of rw 1 - us, 2 33.8, 4 25.7, 8 28.7; 512 tokens 9.6, 10.9, 11.8, -.  1024 + 4096 rows, 2000 tokens of six slots of rank 64: 24.0, 30.9,
-// 33.3, 43.8.  Rank 64 is read from the cache once for every 16 rw rows, so long sums take rw 2: 34.9 us against 39.5.
+// blocks of 128 tokens.  Shares fill the GPU but cost a launch that joins them, 4 us.  4096 + 4096 rows of one slot, 1 / 2 / 4 / 8 shares:
+// 4096 tokens 38.4 / 26.5 / 22.7 / 24.0 us, 512 10.2 / 11.2 / 11.5 / 14.2.  1024 + 4096 rows, 2000 tokens of six slots of rank 64: 29.8 /
+// 35.0 / 35.4 / 44.6.  Rank 64 is read from the cache once for every 16 rw rows, so long sums take rw 2: 34.9 us against 39.3.
 struct GradShape {
     int rw, tiles_k, tiles_m, splits;
 };

@@ -418,14 +418,14 @@ template <typename T> __global__ __launch_bounds__(256) void k8_turn(const K8Tur
     const int b = (int)blockIdx.x, at = (int)blockIdx.y, side = (int)blockIdx.z / tiles_all, r = (int)blockIdx.z - side * tiles_all, t0 = b * 128;
     // u of the tokens, whatever their slots: one latency for all loads.  What no token of the slot's wrote is taken out below
     const int j4 = lane & 3, q = lane >> 2;
-    const float* p = a.w[side] + kx_at(t0 + 8 * q, r * 16 + wave * 4, a.rank_pad) + j4;      // tokens of a group of eight follow each other
+    const int t8 = min(t0 + 8 * q, (a.n - 1) & ~7);
+    const float* p = a.w[side] + kx_at(t8, r * 16 + wave * 4, a.rank_pad) + j4;      // tokens of a group of eight follow each other
     const int64_t share = kx_share(a.n, a.rank_pad);
     float v[8];
     for (int sp = 0; sp < a.splits[side]; ++sp)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            float x = 0.0f;
-            if (t0 + 8 * q + i < a.n) x = p[sp * share + i * 4];
+            const float x = p[sp * share + i * 4];
             v[i] = sp ? v[i] + x : x;
         }
     const int32_t s0 = t0 + lane < a.n ? a.slot_of[t0 + lane] : -1, s1 = t0 + 64 + lane < a.n ? a.slot_of[t0 + 64 + lane] : -1;
@@ -500,6 +500,13 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
     if (row0 >= rows) return;
     const int at = (int)blockIdx.y, split = (int)blockIdx.z;
     const int tiles_all = a.rank_pad / 16;
+    // No branch stands between z's loads.  Rows that are not there are the last one's; tokens that are not there whatever follows, up to
+    // the matrix's end, and are masked.  Rows of which an eighth of a block has tokens both before and behind that end read the last block twice.
+    const T* const z_all = static_cast<const T*>(of_a ? a.x : a.g);
+    const int64_t z_size = (int64_t)rows * a.n;
+    const T* const z_from = z_size < 8 ? static_cast<const T*>(a.in.w) : z_all;             // (too few to read eight: any memory)
+    const int64_t z_most = z_size < 8 ? 0 : z_size - 8;
+    const bool z_again = !(HELD8 && of_a) && (int64_t)min(row0 + 16 * RW - 1, rows - 1) * a.n + (a.n + 7) / 8 * 8 > z_size;
     const K8Mask* masks = a.in.masks + (int64_t)at * a.blocks;
 
     // 64 blocks at a time, one to a lane
@@ -552,21 +559,26 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
             const int tb = b * 128;
 #pragma unroll
             for (int i = 0; i < RW; ++i) {
-                const int row = row0 + i * 16 + c;
-                const bool row_ok = row < rows;
+                const int row = min(row0 + i * 16 + c, rows - 1);
                 if (HELD8 && of_a) {
                     // 32 bytes of a row to a lane: product st takes tokens 32 g + 8 st .., not 32 st + 8 g .. as otherwise
                     const uint4* src = reinterpret_cast<const uint4*>(static_cast<const int8_t*>(a.x) + (int64_t)row * a.x_pitch + tb + g * 32);
-                    z8[i][0] = z8[i][1] = uint4{0u, 0u, 0u, 0u};
-                    if (row_ok) z8[i][0] = src[0], z8[i][1] = src[1];
-                    const int r4 = row0 + i * 16 + 4 * g;
-                    zs[i] = 0;
-                    if (r4 < a.x_scale_pitch) zs[i] = *reinterpret_cast<const uint32_t*>(a.x_scale + (int64_t)b * a.x_scale_pitch + r4);
+                    z8[i][0] = src[0], z8[i][1] = src[1];
+                    const int64_t r4 = min((int64_t)(row0 + i * 16 + 4 * g), a.x_scale_pitch - 4);
+                    zs[i] = *reinterpret_cast<const uint32_t*>(a.x_scale + (int64_t)b * a.x_scale_pitch + r4);
                 } else {
-                    const T* src = static_cast<const T*>(of_a ? a.x : a.g) + (int64_t)row * a.n + tb + g * 8;
+                    const int64_t from = (int64_t)row * a.n + tb + g * 8;
 #pragma unroll
-                    for (int st = 0; st < 4; ++st) z[i][st] = k8_load<T, 8>(src + st * 32, row_ok ? a.n - (tb + st * 32 + g * 8) : 0);
+                    for (int st = 0; st < 4; ++st) z[i][st] = *reinterpret_cast<const k8_any<T, 8>*>(z_from + min(from + st * 32, z_most));
                 }
+            }
+        };
+        auto load_z_again = [&](int b) {
+#pragma unroll
+            for (int i = 0; i < RW; ++i) {
+                const int row = min(row0 + i * 16 + c, rows - 1), t = b * 128 + g * 8;
+#pragma unroll
+                for (int st = 0; st < 4; ++st) z[i][st] = k8_load<T, 8>(z_all + (int64_t)row * a.n + t + st * 32, a.n - t - st * 32);
             }
         };
 
@@ -590,6 +602,9 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
             const K8Mask mask = masks[b];
             const uint64_t m0 = mask.half[0], m1 = mask.half[1];
             const bool whole = (m0 & m1) == ~0ull;
+            if constexpr (decltype(last)::value) {
+                if (z_again && b == a.blocks - 1) load_z_again(b);
+            }
             k8_v8<T> cur[RW][4];
             float scales[RW][4];
 #pragma unroll

@@ -178,7 +178,6 @@ __global__ __launch_bounds__(64 * kProjectWaves) void k8_project(const K8Project
             }
         }
     };
-    const int full = min(w1, a.rows / 32);                       // steps from here on lack rows: the last one at most
 
     // One slot's tokens (slot -1: only the gate), ranks from tile rt0 on.
     auto pass = [&](int slot, int rt0, int tiles, bool is_first) {
@@ -210,7 +209,7 @@ __global__ __launch_bounds__(64 * kProjectWaves) void k8_project(const K8Project
                 }
                 __builtin_amdgcn_sched_barrier(0);
             };
-            constexpr int P = decltype(whole)::value ? kAhead : 1;      // (the step that lacks rows is one)
+            constexpr int P = kAhead;
             Rows r[P];
 #pragma unroll
             for (int j = 0; j < P; ++j) fetch(min(from + j, to - 1), r[j]);
@@ -233,11 +232,13 @@ __global__ __launch_bounds__(64 * kProjectWaves) void k8_project(const K8Project
                 if (st + P + j < to) multiply(st + P + j, r[j]);
         };
         auto all = [&](auto write_g) {
-            if (w0 < full) steps(std::true_type{}, write_g, w0, full);
-            if (max(w0, full) < w1) steps(std::false_type{}, write_g, max(w0, full), w1);
+            if (w1 * 32 <= a.rows) steps(std::true_type{}, write_g, w0, w1);
+            else steps(std::false_type{}, write_g, w0, w1);
         };
-        if (GATED && is_first && blockIdx.y == 0) all(std::integral_constant<bool, GATED>{});
-        else all(std::false_type{});
+        if (w0 < w1) {
+            if (GATED && is_first && blockIdx.y == 0) all(std::integral_constant<bool, GATED>{});
+            else all(std::false_type{});
+        }
         if (slot < 0) return;
         const int rank = a.rank[slot];
 #pragma unroll

@@ -590,17 +590,24 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
             const int64_t part_of = ((int64_t)at * 2 + (of_a ? 0 : 1)) * a.blocks + b;
             const k8_v8<T>* ops = static_cast<const k8_v8<T>*>(a.in.w) + (part_of * tiles_all + rt0) * 4 * PARTS * 64 + lane;
             const float* downs = a.in.down + part_of * a.rank_pad + rt0 * 16 + c;
-            k8_v8<T> op[RG > 1 ? 2 : 1][4][PARTS];               // of one rank tile, and of the next
-            float down[2] = {1.0f, 1.0f};
+            // w of all rank tiles at once, or, beside two row tiles for which the registers do not suffice, of one and of the next
+            constexpr int OPS = RW == 1 ? RG : 2;
+            k8_v8<T> op[OPS][4][PARTS];
+            float down[OPS];
+#pragma unroll
+            for (int r = 0; r < OPS; ++r) down[r] = 1.0f;
             auto load_op = [&](int r) {
 #pragma unroll
                 for (int st = 0; st < 4; ++st)
 #pragma unroll
-                    for (int part = 0; part < PARTS; ++part) op[r & 1][st][part] = ops[((r * 4 + st) * PARTS + part) * 64];
-                if (half) down[r & 1] = downs[r * 16];
+                    for (int part = 0; part < PARTS; ++part) op[r % OPS][st][part] = ops[((r * 4 + st) * PARTS + part) * 64];
+                if (half) down[r % OPS] = downs[r * 16];
             };
             load_op(0);
             const K8Mask mask = masks[b];
+#pragma unroll
+            for (int r = 1; r < RG; ++r)
+                if (OPS == RG && r < tiles) load_op(r);
             const uint64_t m0 = mask.half[0], m1 = mask.half[1];
             const bool whole = (m0 & m1) == ~0ull;
             if constexpr (decltype(last)::value) {
@@ -639,7 +646,7 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
 #pragma unroll
             for (int r = 0; r < RG; ++r)
                 if (r < tiles) {
-                    if (r + 1 < RG && r + 1 < tiles) load_op(r + 1);
+                    if (OPS < RG && r + 1 < tiles) load_op(r + 1);
                     k8_f4 sum[RW];
 #pragma unroll
                     for (int i = 0; i < RW; ++i) sum[i] = k8_f4(0.0f);
@@ -648,11 +655,11 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
 #pragma unroll
                         for (int part = 0; part < PARTS; ++part)
 #pragma unroll
-                            for (int i = 0; i < RW; ++i) sum[i] = k8_mfma(cur[i][st], op[r & 1][st][part], sum[i]);
+                            for (int i = 0; i < RW; ++i) sum[i] = k8_mfma(cur[i][st], op[r % OPS][st][part], sum[i]);
 #pragma unroll
                     for (int i = 0; i < RW; ++i)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][r][e] = __builtin_fmaf(sum[i][e] * down[r & 1], scales[i][e], acc[i][r][e]);
+                        for (int e = 0; e < 4; ++e) acc[i][r][e] = __builtin_fmaf(sum[i][e] * down[r % OPS], scales[i][e], acc[i][r][e]);
                 }
         };
         for (int done = 0; done + 1 < todo; ++done) block(std::false_type{});

@@ -61,6 +61,13 @@ pp_status_t pp_adapter_plan(const pp_adapter_desc_t *desc, pp_adapter_bank_t **o
  * range.  PP_ERR_UNSUPPORTED: a scale that is not finite. */
 pp_status_t pp_adapter_load(pp_adapter_bank_t *bank, int32_t slot, int32_t rank, float scale, const void *a_dev, const void *b_dev, void *hip_stream);
 
+/* Enqueue the loading of count slots, as count calls of pp_adapter_load in their order would, in a launch for each 64 of them
+ * (fewer where a slot is listed twice: the last of its entries stays).  The five arrays are host memory, count entries each, read before
+ * the call returns; a_dev and b_dev list device pointers, not read where rank is 0.  If one entry is refused, nothing is loaded.
+ * Refusals as pp_adapter_load; PP_ERR_SHAPE also: count < 1. */
+pp_status_t pp_adapter_load_many(pp_adapter_bank_t *bank, int32_t count, const int32_t *slot, const int32_t *rank, const float *scale,
+                                 const void *const *a_dev, const void *const *b_dev, void *hip_stream);
+
 /* Sizes of what a run leaves for the backward pass, for n tokens: u (of A x) and v (of B^T g), opaque, 16-byte aligned.
  * A buffer belongs to the n it was made for.  0 if n is out of range. */
 int64_t pp_adapter_u_bytes(const pp_adapter_bank_t *bank, int32_t n);

@@ -12,6 +12,6 @@ from .autotune import autotune, default_candidates
 from .pp_block_gemm import (BlockPlan, block_plan_from_layer, block_plan_transposed_from_layer, pp_block_gemm_plan, pp_block_gemm_plan_transposed, pp_block_gemm_run, pp_block_gemm_destroy,
                             pp_block_gemm_query, pp_block_gemm_unpack)
 from .pp_deep_reuse import (ReusePlan, reuse_plan_from_layer, pp_reuse_plan, pp_reuse_run, pp_reuse_read_clusters, pp_reuse_destroy)
-from .pp_adapter import (AdapterBank, Act8, InputGradient, act8_pack, pp_act8_bytes, pp_act8_pack, pp_act8_unpack, pp_adapter_plan, pp_adapter_load,
+from .pp_adapter import (AdapterBank, Act8, InputGradient, act8_pack, pp_act8_bytes, pp_act8_pack, pp_act8_unpack, pp_adapter_plan, pp_adapter_load, pp_adapter_load_many,
                          pp_adapter_u_bytes, pp_adapter_v_bytes, pp_adapter_work_bytes, pp_adapter_project, pp_adapter_run, pp_adapter_grad_input,
                          pp_adapter_grad_weights, pp_adapter_destroy)

@@ -54,6 +54,26 @@ pp_status_t plan_fits(const pp_adapter_bank_t* b, const pp_block_gemm_plan_t* pl
 
 // ---- launches (everything has been checked) ----
 
+// n <= N slots, none twice, ranks up to `top`
+template <typename T, int N>
+void load_slots(const pp_adapter_bank_t* b, int n, int top, const int32_t* slot, const int32_t* rank, const float* scale, const void* const* a_dev,
+                const void* const* b_dev, hipStream_t stream) {
+    K8Load<N> p{};
+    p.a_project = b->a_project, p.b_project = b->b_project, p.a_expand = b->a_expand, p.b_expand = b->b_expand;
+    const int64_t eb = elem(b);
+    p.a_project_slot = b->a_project_slot / eb, p.b_project_slot = b->b_project_slot / eb;
+    p.a_expand_slot = b->a_expand_slot / eb, p.b_expand_slot = b->b_expand_slot / eb;
+    p.rank = b->rank, p.scale = b->scale;
+    p.m = b->m, p.k = b->k, p.rank_pad = b->rank_pad;
+    for (int i = 0; i < n; ++i) p.of[i] = K8LoadSlot{a_dev[i], b_dev[i], scale[i], rank[i], slot[i], 0};
+    const int pad = adapter_rank_pad(top);
+    const bool half = sizeof(T) == 2;
+    const int64_t items = (adapter_project_elems(b->k, pad) + adapter_project_elems(b->m, pad) + adapter_expand_elems(b->k, pad, half) +
+                           adapter_expand_elems(b->m, pad, half)) / 8, wgs = (items + 255) / 256;
+    const unsigned grid = wgs < 1 ? 1u : (wgs < 65536 ? (unsigned)wgs : 65536u);
+    hipLaunchKernelGGL((k8_load_slots<T, N>), dim3(grid, (unsigned)n), dim3(256), 0, stream, p);
+}
+
 template <typename T, int FT, int RG, bool GATED> void project_as(const K8Project& a, dim3 grid, hipStream_t stream) {
     hipLaunchKernelGGL((k8_project<T, FT, RG, GATED>), grid, dim3(64 * kProjectWaves), 0, stream, a);
 }
@@ -178,29 +198,43 @@ pp_status_t pp_adapter_plan(const pp_adapter_desc_t* desc, pp_adapter_bank_t** o
     return PP_OK;
 }
 
-pp_status_t pp_adapter_load(pp_adapter_bank_t* bank, int32_t slot, int32_t rank, float scale, const void* a_dev, const void* b_dev, void* hip_stream) {
-    if (!bank || (rank != 0 && (!a_dev || !b_dev))) return PP_ERR_NULL;
-    if (slot < 0 || slot >= bank->slots || rank < 0 || rank > bank->max_rank) return PP_ERR_SHAPE;
-    if (!std::isfinite(scale)) return PP_ERR_UNSUPPORTED;
-    if (rank && (misaligned(a_dev) || misaligned(b_dev))) return PP_ERR_ALIGN;
+pp_status_t pp_adapter_load_many(pp_adapter_bank_t* bank, int32_t count, const int32_t* slot, const int32_t* rank, const float* scale,
+                                 const void* const* a_dev, const void* const* b_dev, void* hip_stream) {
+    if (!bank || !slot || !rank || !scale || !a_dev || !b_dev) return PP_ERR_NULL;
+    if (count < 1) return PP_ERR_SHAPE;
+    for (int32_t i = 0; i < count; ++i) {
+        if (rank[i] != 0 && (!a_dev[i] || !b_dev[i])) return PP_ERR_NULL;
+        if (slot[i] < 0 || slot[i] >= bank->slots || rank[i] < 0 || rank[i] > bank->max_rank) return PP_ERR_SHAPE;
+        if (!std::isfinite(scale[i])) return PP_ERR_UNSUPPORTED;
+        if (rank[i] && (misaligned(a_dev[i]) || misaligned(b_dev[i]))) return PP_ERR_ALIGN;
+    }
     const pp_status_t st = ready(bank);
     if (st != PP_OK) return st;
-    K8Load p{};
-    p.a = a_dev, p.b = b_dev;
-    p.a_project = bank->a_project + slot * bank->a_project_slot, p.b_project = bank->b_project + slot * bank->b_project_slot;
-    p.a_expand = bank->a_expand + slot * bank->a_expand_slot, p.b_expand = bank->b_expand + slot * bank->b_expand_slot;
-    p.rank = bank->rank, p.scale = bank->scale, p.factor = scale;
-    p.m = bank->m, p.k = bank->k, p.r = rank, p.rank_pad = bank->rank_pad, p.slot = slot;
-    const int tiles = (rank + 15) / 16;
-    const bool half = bank->dtype == PP_F16;
-    p.items[0] = adapter_project_elems(bank->k, tiles * 16) / 8, p.items[1] = adapter_project_elems(bank->m, tiles * 16) / 8;
-    p.items[2] = adapter_expand_elems(bank->k, tiles * 16, half) / 8, p.items[3] = adapter_expand_elems(bank->m, tiles * 16, half) / 8;
-    const int64_t wgs = (p.items[0] + p.items[1] + p.items[2] + p.items[3] + 255) / 256;
-    const unsigned grid = wgs < 1 ? 1u : (wgs < 65536 ? (unsigned)wgs : 65536u);
     (void)hipGetLastError();
-    if (half) hipLaunchKernelGGL(k8_load_slot<_Float16>, dim3(grid), dim3(256), 0, static_cast<hipStream_t>(hip_stream), p);
-    else hipLaunchKernelGGL(k8_load_slot<float>, dim3(grid), dim3(256), 0, static_cast<hipStream_t>(hip_stream), p);
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    for (int32_t from = 0; from < count;) {
+        // up to kAdapterLoads slots, none of them twice: their loads have no order within a launch
+        int n = 0, top = 0;
+        for (; n < kAdapterLoads && from + n < count; ++n) {
+            bool again = false;
+            for (int i = 0; i < n; ++i) again = again || slot[from + i] == slot[from + n];
+            if (again) break;
+            top = rank[from + n] > top ? rank[from + n] : top;
+        }
+        if (bank->dtype == PP_F16) {
+            if (n == 1) load_slots<_Float16, 1>(bank, 1, top, slot + from, rank + from, scale + from, a_dev + from, b_dev + from, stream);
+            else load_slots<_Float16, kAdapterLoads>(bank, n, top, slot + from, rank + from, scale + from, a_dev + from, b_dev + from, stream);
+        } else {
+            if (n == 1) load_slots<float, 1>(bank, 1, top, slot + from, rank + from, scale + from, a_dev + from, b_dev + from, stream);
+            else load_slots<float, kAdapterLoads>(bank, n, top, slot + from, rank + from, scale + from, a_dev + from, b_dev + from, stream);
+        }
+        from += n;
+    }
     return launched();
+}
+
+pp_status_t pp_adapter_load(pp_adapter_bank_t* bank, int32_t slot, int32_t rank, float scale, const void* a_dev, const void* b_dev, void* hip_stream) {
+    return pp_adapter_load_many(bank, 1, &slot, &rank, &scale, &a_dev, &b_dev, hip_stream);
 }
 
 int64_t pp_adapter_u_bytes(const pp_adapter_bank_t* bank, int32_t n) { return bank && tokens_ok(bank, n) ? adapter_state_bytes(bank->k, n, bank->rank_pad, bank->dtype == PP_F16, false) : 0; }

@@ -4,6 +4,12 @@
 
 #include <cstdint>
 
+#if defined(__HIP__)
+#define PP_HOST_DEVICE __host__ __device__
+#else
+#define PP_HOST_DEVICE
+#endif
+
 namespace ppc {
 
 constexpr int kAct8Block = 128;                 // columns that share a scale
@@ -18,11 +24,13 @@ inline int64_t act8_bytes(int64_t rows, int64_t n) { return rows * act8_pitch(n)
 
 inline int adapter_rank_pad(int max_rank) { return (max_rank + 15) / 16 * 16; }
 
+constexpr int kAdapterLoads = 64;               // slots that one launch loads at most
+
 // Elements of one slot's matrix (a rank x width one, or its transpose) in the two orders kept of it:
 // for projections [rank / 16][width / 32][64 lanes][8], for expansions (binary16) [width / 64][rank / 16][2][64 lanes][8] or
 // (binary32) [width][rank].
-inline int64_t adapter_project_elems(int width, int rank_pad) { return (int64_t)(rank_pad / 16) * ((width + 31) / 32) * 512; }
-inline int64_t adapter_expand_elems(int width, int rank_pad, bool half) {
+PP_HOST_DEVICE inline int64_t adapter_project_elems(int width, int rank_pad) { return (int64_t)(rank_pad / 16) * ((width + 31) / 32) * 512; }
+PP_HOST_DEVICE inline int64_t adapter_expand_elems(int width, int rank_pad, bool half) {
     return half ? (int64_t)((width + 63) / 64) * (rank_pad / 16) * 1024 : (int64_t)width * rank_pad;
 }
 

@@ -34,28 +34,41 @@ __device__ __forceinline__ k8_f4 k8_mfma(const k8_v8<float>& a, const k8_v8<floa
 }
 
 // ---- loading ----
-// Copies A [rank][k] and B [m][rank] into operand order for both directions, zeros behind the rank and the sizes, one lane to
-// eight values.  Only the ranks' tiles of 16 that the rank reaches are written: no kernel reads the others.
-struct K8Load {
+// Copies A [rank][k] and B [m][rank] of up to N slots into operand order for both directions, zeros behind the rank and the sizes, one lane
+// to eight values.  Only the ranks' tiles of 16 that the rank reaches are written: no kernel reads the others.  The slots are arguments of
+// the kernel, 32 bytes each: no table has to reach the device first.  What a single load costs is its launch: 64 slots of rank 16 take 4.3 us
+// in a launch and 174 in one each with 300 x 300, 24 and 187 with 4096 x 4096.  N = 1 is there because 2 KB of arguments cost the host
+// 0.5 us: a call of one slot takes 6.8 us, 7.3 with room for 64.
+struct K8LoadSlot {
     const void* a;
     const void* b;
-    void *a_project, *b_project;     // A and B^T, rows = ranks
+    float factor;
+    int32_t r, slot, unused;
+};
+template <int N> struct K8Load {
+    void *a_project, *b_project;     // A and B^T, rows = ranks: slot 0's
     void *a_expand, *b_expand;       // A^T and B, rows = k and m
+    int64_t a_project_slot, b_project_slot, a_expand_slot, b_expand_slot;     // elements of one slot
     int32_t* rank;
     float* scale;
-    float factor;
-    int32_t m, k, r, rank_pad, slot;
-    int64_t items[4];                // eights of a_project, b_project, a_expand, b_expand
+    int32_t m, k, rank_pad;
+    K8LoadSlot of[N];
 };
-template <typename T> __global__ __launch_bounds__(256) void k8_load_slot(const K8Load p) {
-    if (blockIdx.x == 0 && threadIdx.x == 0) p.rank[p.slot] = p.r, p.scale[p.slot] = p.factor;
-    const T* a = static_cast<const T*>(p.a);
-    const T* b = static_cast<const T*>(p.b);
+template <typename T, int N> __global__ __launch_bounds__(256) void k8_load_slots(const K8Load<N> p) {
+    const K8LoadSlot s = p.of[N == 1 ? 0 : blockIdx.y];
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.rank[s.slot] = s.r, p.scale[s.slot] = s.factor;
+    const T* a = static_cast<const T*>(s.a);
+    const T* b = static_cast<const T*>(s.b);
     constexpr bool half = sizeof(T) == 2;
+    const int tiles = (s.r + 15) / 16;                           // of the rank: the ones written
+    const int64_t items[4] = {adapter_project_elems(p.k, tiles * 16) / 8, adapter_project_elems(p.m, tiles * 16) / 8,
+                              adapter_expand_elems(p.k, tiles * 16, half) / 8, adapter_expand_elems(p.m, tiles * 16, half) / 8};
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;; at += (int64_t)gridDim.x * 256) {
         int64_t i = at;
         int what = 0;
-        while (what < 4 && i >= p.items[what]) i -= p.items[what++];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (what == q && i >= items[q]) i -= items[q], ++what;
         if (what == 4) break;
         const bool of_a = (what & 1) == 0;
         const int width = of_a ? p.k : p.m;
@@ -68,29 +81,29 @@ template <typename T> __global__ __launch_bounds__(256) void k8_load_slot(const 
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 T x = (T)0.0f;
-                if (row < p.r && c0 + e < width) x = of_a ? a[(int64_t)row * p.k + c0 + e] : b[(int64_t)(c0 + e) * p.r + row];
+                if (row < s.r && c0 + e < width) x = of_a ? a[(int64_t)row * p.k + c0 + e] : b[(int64_t)(c0 + e) * s.r + row];
                 v[e] = x;
             }
-            dst = static_cast<T*>(of_a ? p.a_project : p.b_project) + i * 8;
+            dst = static_cast<T*>(of_a ? p.a_project : p.b_project) + s.slot * (of_a ? p.a_project_slot : p.b_project_slot) + i * 8;
         } else {
-            const int tiles = (p.r + 15) / 16;                   // of the rank: the ones written
             int row, j0;
+            dst = static_cast<T*>(of_a ? p.a_expand : p.b_expand) + s.slot * (of_a ? p.a_expand_slot : p.b_expand_slot);
             if (half) {                                          // [width / 64][rank_pad / 16][2][64][8]
                 const int lane = (int)(i & 63), side = (int)(i >> 6) & 1;
                 const int64_t group = i >> 7;
                 const int64_t tile = group / tiles;
                 const int chunk = (int)(group - tile * tiles);
                 row = (int)tile * 64 + side * 32 + (lane & 31), j0 = chunk * 16 + (lane >> 5) * 8;
-                dst = static_cast<T*>(of_a ? p.a_expand : p.b_expand) + (((tile * (p.rank_pad / 16) + chunk) * 2 + side) * 64 + lane) * 8;
+                dst += (((tile * (p.rank_pad / 16) + chunk) * 2 + side) * 64 + lane) * 8;
             } else {                                             // [width][rank_pad]
                 const int64_t eighth = i / (2 * tiles);
                 row = (int)eighth, j0 = (int)(i - eighth * (2 * tiles)) * 8;
-                dst = static_cast<T*>(of_a ? p.a_expand : p.b_expand) + (int64_t)row * p.rank_pad + j0;
+                dst += (int64_t)row * p.rank_pad + j0;
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 T x = (T)0.0f;
-                if (row < width && j0 + e < p.r) x = of_a ? a[(int64_t)(j0 + e) * p.k + row] : b[(int64_t)row * p.r + j0 + e];
+                if (row < width && j0 + e < s.r) x = of_a ? a[(int64_t)(j0 + e) * p.k + row] : b[(int64_t)row * s.r + j0 + e];
                 v[e] = x;
             }
         }

@@ -3,7 +3,8 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
-from typing import NamedTuple, Optional, Union
+from array import array
+from typing import NamedTuple, Optional, Sequence, Union
 
 from .pp_block_gemm import BlockPlan, lib as _block_lib
 from .pp_conv import PP_OK, PP_F16, PP_F32, PP_FLAG_HOST_ONLY, PPError
@@ -27,6 +28,7 @@ def lib() -> C.CDLL:
             "pp_act8_unpack": [vp, i32, i32, i32, vp, vp],
             "pp_adapter_plan": [C.POINTER(_Desc), C.POINTER(vp)],
             "pp_adapter_load": [vp, i32, i32, C.c_float, vp, vp, vp],
+            "pp_adapter_load_many": [vp, i32, vp, vp, vp, vp, vp, vp],
             "pp_adapter_project": [vp, vp, vp, vp, i32, vp],
             "pp_adapter_run": [vp, vp, vp, vp, vp, vp, i32, vp],
             "pp_adapter_grad_input": [vp, vp, vp, vp, vp, vp, vp, vp, i32, vp],
@@ -69,6 +71,13 @@ def pp_adapter_plan(m: int, k: int, slots: int, max_rank: int, dtype: int = PP_F
 
 def pp_adapter_load(bank, slot: int, rank: int, scale: float, a_dev: int, b_dev: int, hip_stream: int = 0) -> int:
     return lib().pp_adapter_load(bank, slot, rank, scale, a_dev, b_dev, hip_stream)
+
+
+def pp_adapter_load_many(bank, slots, ranks, scales, a_dev, b_dev, hip_stream: int = 0) -> int:
+    """The five sequences have one entry a slot; 0 stands for a null pointer."""
+    assert len(slots) == len(ranks) == len(scales) == len(a_dev) == len(b_dev)
+    lists = array("i", slots), array("i", ranks), array("f", scales), array("Q", a_dev), array("Q", b_dev)
+    return lib().pp_adapter_load_many(bank, len(slots), *[t.buffer_info()[0] for t in lists], hip_stream)
 
 
 def pp_adapter_u_bytes(bank, n: int) -> int:
@@ -244,6 +253,21 @@ class AdapterBank:
         _matrix(b, self.m, rank, self.dtype, self.device)
         _on(self.device, stream, lambda s: _check_status(
             lib().pp_adapter_load(self.handle, slot, rank, scale, a.data_ptr(), b.data_ptr(), s), "pp_adapter_load"))
+
+    def load_many(self, slots: Sequence[int], a, b, scales: Sequence[float], stream: Optional[int] = None) -> None:
+        """a[i] [rank, k] and b[i] [m, rank] into slots[i], for all i in one call (in their order, where a slot stands twice; no slots: nothing)."""
+        assert len(slots) == len(a) == len(b) == len(scales)
+        if not len(slots):
+            return
+        tdt, index, t = _torch_dtype(self.dtype), self.device.index, _TORCH.Tensor
+        both = [*a, *b]                            # a list of 64 slots takes 60 us to look over one tensor after another, 45 check by check
+        sizes = list(map(t.size, a))
+        ranks = [s[0] if len(s) == 2 else -1 for s in sizes]
+        assert sizes == [(r, self.k) for r in ranks] and list(map(t.size, b)) == [(self.m, r) for r in ranks]
+        assert all([x.dtype is tdt for x in both]) and set(map(t.get_device, both)) == {index} and all(map(t.is_contiguous, both))
+        at = list(map(t.data_ptr, both))
+        _on(self.device, stream, lambda s: _check_status(
+            pp_adapter_load_many(self.handle, slots, ranks, scales, at[:len(a)], at[len(a):], s), "pp_adapter_load_many"))
 
     def unload(self, slot: int, stream: Optional[int] = None) -> None:
         _on(self.device, stream, lambda s: _check_status(lib().pp_adapter_load(self.handle, slot, 0, 0.0, None, None, s), "pp_adapter_load"))

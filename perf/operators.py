@@ -240,8 +240,7 @@ def run(state):
 
 def _run_adapted(st):
     if st.case["load"]:
-        for s in st.used:
-            st.bank.load(s, st.a[s], st.b[s], st.scale[s])
+        st.bank.load_many(st.used, [st.a[s] for s in st.used], [st.b[s] for s in st.used], [st.scale[s] for s in st.used])
     return st.bank.run(st.plan, st.x, st.slot_of)
 
 

@@ -141,20 +141,13 @@ pp_status_t act8_check(const void* x_dev, int32_t rows, int32_t n, int32_t dtype
     return xa < he && ha < xe ? PP_ERR_ALIGN : PP_OK;
 }
 
-Act8Args act8_args(const void* x_dev, int32_t rows, int32_t n, void* held_dev) {
+Act8Args act8_args(const Act8Shape& sh, const void* x_dev, int32_t rows, int32_t n, void* held_dev) {
     Act8Args a;
     a.x = x_dev, a.q = static_cast<int8_t*>(held_dev);
-    a.rows = rows, a.n = n, a.blocks = (n + kAct8Block - 1) / kAct8Block;
+    a.rows = rows, a.n = n, a.blocks = sh.blocks, a.runs = sh.runs, a.units = sh.units;
     a.pitch = act8_pitch(n), a.scale_pitch = act8_scale_pitch(rows);
     a.scale = static_cast<uint8_t*>(held_dev) + rows * a.pitch;
-    a.runs = (a.blocks + kAct8Ahead - 1) / kAct8Ahead;
-    a.units = (int64_t)rows * a.runs;
     return a;
-}
-
-unsigned act8_grid(const Act8Args& a) {
-    const int64_t wgs = (a.units + 15) / 16;
-    return (unsigned)(wgs < (1 << 20) ? wgs : (1 << 20));
 }
 
 }  // namespace
@@ -169,20 +162,22 @@ int64_t pp_act8_bytes(int32_t rows, int32_t n) {
 pp_status_t pp_act8_pack(const void* x_dev, int32_t rows, int32_t n, int32_t dtype, void* held_dev, void* hip_stream) {
     const pp_status_t st = act8_check(x_dev, rows, n, dtype, held_dev);
     if (st != PP_OK) return st;
-    const Act8Args a = act8_args(x_dev, rows, n, held_dev);
+    const Act8Shape sh = act8_shape(rows, n, kAct8Ahead);
+    const Act8Args a = act8_args(sh, x_dev, rows, n, held_dev);
     (void)hipGetLastError();
-    if (dtype == PP_F16) hipLaunchKernelGGL(act8_pack<_Float16>, dim3(act8_grid(a)), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
-    else hipLaunchKernelGGL(act8_pack<float>, dim3(act8_grid(a)), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
+    if (dtype == PP_F16) hipLaunchKernelGGL(act8_pack<_Float16>, dim3(sh.wgs), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
+    else hipLaunchKernelGGL(act8_pack<float>, dim3(sh.wgs), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
     return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_DEVICE;
 }
 
 pp_status_t pp_act8_unpack(const void* held_dev, int32_t rows, int32_t n, int32_t dtype, void* x_dev, void* hip_stream) {
     const pp_status_t st = act8_check(x_dev, rows, n, dtype, held_dev);
     if (st != PP_OK) return st;
-    const Act8Args a = act8_args(x_dev, rows, n, const_cast<void*>(held_dev));
+    const Act8Shape sh = act8_shape(rows, n, kAct8Ahead);
+    const Act8Args a = act8_args(sh, x_dev, rows, n, const_cast<void*>(held_dev));
     (void)hipGetLastError();
-    if (dtype == PP_F16) hipLaunchKernelGGL(act8_unpack<_Float16>, dim3(act8_grid(a)), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
-    else hipLaunchKernelGGL(act8_unpack<float>, dim3(act8_grid(a)), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
+    if (dtype == PP_F16) hipLaunchKernelGGL(act8_unpack<_Float16>, dim3(sh.wgs), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
+    else hipLaunchKernelGGL(act8_unpack<float>, dim3(sh.wgs), dim3(256), 0, static_cast<hipStream_t>(hip_stream), a);
     return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_DEVICE;
 }
 

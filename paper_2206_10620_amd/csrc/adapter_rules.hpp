@@ -22,6 +22,23 @@ inline int64_t act8_pitch(int64_t n) { return (n + kAct8Block - 1) / kAct8Block 
 inline int64_t act8_scale_pitch(int64_t rows) { return (rows + 15) / 16 * 16; }
 inline int64_t act8_bytes(int64_t rows, int64_t n) { return rows * act8_pitch(n) + act8_pitch(n) / kAct8Block * act8_scale_pitch(rows); }
 
+// How the rows are gone through: sixteen lanes take `ahead` blocks of a row at a time, a unit; a workgroup sixteen units.  n may be 2^31 - 1:
+// rounded up it passes 31 bits.
+struct Act8Shape {
+    int blocks, runs;           // of a row: blocks, and units
+    int64_t units;
+    unsigned wgs;
+};
+inline Act8Shape act8_shape(int32_t rows, int32_t n, int ahead) {
+    Act8Shape s;
+    s.blocks = (int)(act8_pitch(n) / kAct8Block);
+    s.runs = (s.blocks + ahead - 1) / ahead;
+    s.units = (int64_t)rows * s.runs;
+    const int64_t wgs = (s.units + 15) / 16;
+    s.wgs = (unsigned)(wgs < (1 << 20) ? wgs : (1 << 20));
+    return s;
+}
+
 inline int adapter_rank_pad(int max_rank) { return (max_rank + 15) / 16 * 16; }
 
 constexpr int kAdapterLoads = 64;               // slots that one launch loads at most

@@ -103,6 +103,8 @@ pp_status_t pp_adapter_grad_input(const pp_adapter_bank_t *bank, const pp_block_
  *   db_dev     binary32 [count][m][max_rank], columns from the slot's rank on are zeros
  *   work_dev   pp_adapter_work_bytes bytes of scratch
  * An entry of which_dev outside 0 .. slots - 1, an empty slot and one that no token names get zeros; a slot may be listed twice.
+ * u and v say with which rank and factor they were made, and dB takes those of u, dA those of v: what has been loaded into a slot since
+ * changes nothing.  slot_of_dev has to be as it was then; a token that it names another slot for than u (v) does counts for neither.
  * Sums are taken in an order that follows from the sizes and the tokens' slots: equal calls give equal bits.  PP_ERR_SHAPE also: count < 1 or above 65535. */
 pp_status_t pp_adapter_grad_weights(const pp_adapter_bank_t *bank, const void *x_dev, int32_t x_is_act8, const void *u_dev, const void *g_dev,
                                     const void *v_dev, const int32_t *slot_of_dev, const int32_t *which_dev, int32_t count, float *da_dev, float *db_dev,

@@ -343,8 +343,9 @@ pp_status_t pp_adapter_grad_weights(const pp_adapter_bank_t* bank, const void* x
     t.out = turned;
     t.w[0] = sums_of(v_dev, n), t.w[1] = sums_of(u_dev, n);
     t.splits[0] = project_shape(bank->m, n, half, true).splits, t.splits[1] = project_shape(bank->k, n, half, false).splits;
-    t.slot_of = slot_of_dev, t.which = which_dev, t.rank = bank->rank, t.scale = bank->scale;
-    t.n = n, t.slots = bank->slots, t.blocks = (n + kAct8Block - 1) / kAct8Block, t.rank_pad = bank->rank_pad, t.x_is_act8 = x_is_act8 ? 1 : 0;
+    t.tokens[0] = static_cast<const KxToken*>(v_dev), t.tokens[1] = static_cast<const KxToken*>(u_dev);
+    t.slot_of = slot_of_dev, t.which = which_dev;
+    t.n = n, t.blocks = (n + kAct8Block - 1) / kAct8Block, t.rank_pad = bank->rank_pad, t.x_is_act8 = x_is_act8 ? 1 : 0;
     const dim3 turns((unsigned)t.blocks, (unsigned)count, (unsigned)(2 * (bank->rank_pad / 16)));
     if (half) hipLaunchKernelGGL(k8_turn<_Float16>, turns, dim3(256), 0, stream, t);
     else hipLaunchKernelGGL(k8_turn<float>, turns, dim3(256), 0, stream, t);

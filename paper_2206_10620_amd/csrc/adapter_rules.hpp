@@ -118,8 +118,8 @@ inline GradWork grad_work(int m, int k, int n, int count, int rank_pad, bool hal
     const int64_t blocks = (n + kAct8Block - 1) / kAct8Block;
     const GradShape s = grad_shape(m, k, n, count, rank_pad, half);
     GradWork o;
-    o.masks = (int64_t)count * 16;
-    o.w = o.masks + count * blocks * 16;
+    o.masks = (int64_t)count * 2 * 16;                                   // K8Slot, then K8Mask
+    o.w = o.masks + count * 2 * blocks * 32;
     o.down = o.w + count * 2 * blocks * rank_pad * kAct8Block * 4;       // two binary16 parts or one binary32
     o.sums = o.down + (half ? count * 2 * blocks * rank_pad * 4 : 0);
     o.bytes = o.sums + (s.splits > 1 ? (int64_t)s.splits * count * ((int64_t)m + k) * rank_pad * 4 : 0);

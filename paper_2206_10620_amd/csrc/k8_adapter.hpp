@@ -394,18 +394,23 @@ __global__ __launch_bounds__(256) void k8_expand_f32(const K8Expand a) {
 // two parts, hi and lo, after a power of two taken out for each rank and block; x in 8 bits is exact in binary16, and its power of
 // two for each row and block joins the other when a block's sum is added to the whole.
 
-// What k8_turn leaves, for each slot listed.
-struct K8Slot {
-    int32_t rank;               // 0: nothing to do
+// What k8_turn leaves, for each slot listed and side (v, u) and block.  Rank and factor are those that the projection found, which its tokens'
+// records name: of other ranks nothing stands in v and u, whatever has been loaded into the slot since.
+struct K8Mask {
+    uint64_t half[2];           // which of a block's 128 tokens are the slot's
+    int32_t rank;               // 0: none is
     float factor;
     int32_t unused[2];
 };
-struct K8Mask {
-    uint64_t half[2];           // which of a block's 128 tokens are the slot's
+// and what k8_grad leaves for k8_grad_join
+struct K8Slot {
+    int32_t rank;               // 0: nothing was found
+    float factor;
+    int32_t unused[2];
 };
 struct K8Turned {
-    K8Slot* slots;              // [count]
-    K8Mask* masks;              // [count][blocks]
+    K8Slot* slots;              // [count][2: v, u]
+    K8Mask* masks;              // [count][2][blocks]
     void* w;                    // [count][2: v, u][blocks][rank tile][4][parts][64 lanes][8]
     float* down;                // [count][2][blocks][rank_pad]: undoes the power of two
 };
@@ -413,13 +418,11 @@ template <typename T> constexpr int kK8Parts = sizeof(T) == 2 ? 2 : 1;
 
 struct K8Turn {
     K8Turned out;
-    const KxToken* tokens;
+    const KxToken* tokens[2];   // v's, u's: [n]
     const float* w[2];          // v, u: [splits][kx_share], kx_at
     const int32_t* slot_of;
     const int32_t* which;
-    const int32_t* rank;
-    const float* scale;
-    int32_t n, slots, blocks, rank_pad, splits[2];
+    int32_t n, blocks, rank_pad, splits[2];
     int32_t x_is_act8;          // v's tokens in the order in which lanes take 32 bytes of x: see k8_grad
 };
 
@@ -442,16 +445,24 @@ template <typename T> __global__ __launch_bounds__(256) void k8_turn(const K8Tur
             const float x = p[sp * share + i * 4];
             v[i] = sp ? v[i] + x : x;
         }
-    const int32_t s0 = t0 + lane < a.n ? a.slot_of[t0 + lane] : -1, s1 = t0 + 64 + lane < a.n ? a.slot_of[t0 + 64 + lane] : -1;
     const int wanted = a.which[at];
-    const int slot = (uint32_t)wanted < (uint32_t)a.slots ? wanted : -1;
-    const int rank = slot < 0 ? 0 : __builtin_amdgcn_readfirstlane(a.rank[slot]);
-    const uint64_t m0 = rank > 0 ? __builtin_amdgcn_ballot_w64(s0 == slot) : 0, m1 = rank > 0 ? __builtin_amdgcn_ballot_w64(s1 == slot) : 0;
-    if (blockIdx.z == 0 && threadIdx.x == 0) {
-        a.out.masks[(int64_t)at * a.blocks + b] = K8Mask{{m0, m1}};
-        if (b == 0) a.out.slots[at] = K8Slot{rank, slot < 0 ? 0.0f : a.scale[slot], {0, 0}};
+    KxToken tok[2];
+    uint64_t m[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int t = t0 + h * 64 + lane;
+        tok[h] = KxToken{-1, 0, 0.0f, 0};
+        int32_t named = -1;
+        if (t < a.n) tok[h] = a.tokens[side][t], named = a.slot_of[t];
+        m[h] = __builtin_amdgcn_ballot_w64(wanted >= 0 && named == wanted && tok[h].slot == wanted);
     }
-    if ((m0 | m1) == 0 || r * 16 >= rank) return;
+    const uint64_t m0 = m[0], m1 = m[1];
+    const int first = (int)__builtin_ctzll(m0 ? m0 : (m1 ? m1 : 1));
+    const bool any = (m0 | m1) != 0;
+    const int rank = any ? __builtin_amdgcn_readlane(m0 ? tok[0].rank : tok[1].rank, first) : 0;
+    if (r == 0 && threadIdx.x == (unsigned)first)
+        a.out.masks[((int64_t)at * 2 + side) * a.blocks + b] = K8Mask{{m0, m1}, rank, any ? (m0 ? tok[0].factor : tok[1].factor) : 0.0f, {0, 0}};
+    if (r * 16 >= rank) return;
     const uint32_t byte = (uint32_t)((q < 8 ? m0 : m1) >> (8 * (q & 7))) & 0xffu;
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = (byte >> i) & 1u ? v[i] : 0.0f;
@@ -521,26 +532,32 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
     const T* const z_from = z_size < 8 ? static_cast<const T*>(a.in.w) : z_all;             // (too few to read eight: any memory)
     const int64_t z_most = z_size < 8 ? 0 : z_size - 8;
     const bool z_again = !(HELD8 && of_a) && (int64_t)min(row0 + 16 * RW - 1, rows - 1) * a.n + (a.n + 7) / 8 * 8 > z_size;
-    const K8Mask* masks = a.in.masks + (int64_t)at * a.blocks;
+    const K8Mask* masks = a.in.masks + ((int64_t)at * 2 + (of_a ? 0 : 1)) * a.blocks;
 
-    // 64 blocks at a time, one to a lane
+    // 64 blocks at a time, one to a lane; rank and factor are in every block found: the first one's
+    int rank = 0;
+    float factor = 0.0f;
     auto found = [&](int group) {
         const int b = group * 64 + lane;
-        bool some = false;
-        if (b < a.blocks) some = (masks[b].half[0] | masks[b].half[1]) != 0;
-        return (uint64_t)__builtin_amdgcn_ballot_w64(some);
+        K8Mask mask = {{0, 0}, 0, 0.0f, {0, 0}};
+        if (b < a.blocks) mask = masks[b];
+        const uint64_t some = __builtin_amdgcn_ballot_w64(mask.rank > 0);
+        if (rank == 0 && some) {
+            const int first = (int)__builtin_ctzll(some);
+            const float f = mask.factor;
+            rank = __builtin_amdgcn_readlane(mask.rank, first);
+            factor = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), first));
+        }
+        return some;
     };
     const int groups = (a.blocks + 63) / 64;
-    const uint64_t found0 = found(0);                            // does not wait for the rank
-    const K8Slot slot = a.in.slots[at];
-    const int rank = __builtin_amdgcn_readfirstlane(slot.rank);
+    const uint64_t found0 = found(0);
     int mine = 0, skip = 0;                                      // this workgroup's share of the blocks found
-    if (rank > 0) {
-        int count = __builtin_popcountll(found0);
-        for (int i = 1; i < groups; ++i) count += __builtin_popcountll(found(i));
-        skip = (int)((int64_t)count * split / a.splits);
-        mine = (int)((int64_t)count * (split + 1) / a.splits) - skip;
-    }
+    int count = __builtin_popcountll(found0);
+    for (int i = 1; i < groups; ++i) count += __builtin_popcountll(found(i));
+    skip = (int)((int64_t)count * split / a.splits);
+    mine = (int)((int64_t)count * (split + 1) / a.splits) - skip;
+    if (a.splits > 1 && split == 0 && row0 == 0 && lane == 0) a.in.slots[at * 2 + (of_a ? 0 : 1)] = K8Slot{rank, factor, {0, 0}};
 
     for (int rt0 = 0; rt0 < tiles_all; rt0 += RG) {
         const int tiles = min((rank + 15) / 16 - rt0, RG);       // of this slot, here (none: zeros are stored)
@@ -617,11 +634,10 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
                 if (half) down[r % OPS] = downs[r * 16];
             };
             load_op(0);
-            const K8Mask mask = masks[b];
+            const uint64_t m0 = masks[b].half[0], m1 = masks[b].half[1];
 #pragma unroll
             for (int r = 1; r < RG; ++r)
                 if (OPS == RG && r < tiles) load_op(r);
-            const uint64_t m0 = mask.half[0], m1 = mask.half[1];
             const bool whole = (m0 & m1) == ~0ull;
             if constexpr (decltype(last)::value) {
                 if (z_again && b == a.blocks - 1) load_z_again(b);
@@ -697,7 +713,7 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
                             if (p + e < rows) part[(int64_t)a.rank_pad * a.k + (int64_t)(p + e) * a.rank_pad + j] = v[e];
                 } else if (j < a.max_rank) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = j < rank ? v[e] * slot.factor : 0.0f;
+                    for (int e = 0; e < 4; ++e) v[e] = j < rank ? v[e] * factor : 0.0f;
                     if (of_a) k8_store<float, 4>(a.da + ((int64_t)at * a.max_rank + j) * a.k + p, rows - p, v);
                     else
 #pragma unroll
@@ -710,7 +726,7 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
 
 // Adds the shares up, in order, and takes the slot's factor in.
 struct K8Join {
-    const K8Slot* slots;
+    const K8Slot* slots;        // [count][2]
     const float* work;
     float *da, *db;
     int64_t wgs_a;              // workgroups of 256 values of A's gradient; B's follow
@@ -732,7 +748,7 @@ __global__ __launch_bounds__(256) void k8_grad_join(const K8Join a) {
         src = (int64_t)a.rank_pad * a.k + (row + off / (uint32_t)a.max_rank) * a.rank_pad + j;
     }
     const float* p = a.work + at * per + src;
-    const K8Slot slot = a.slots[at];
+    const K8Slot slot = a.slots[at * 2 + (of_a ? 0 : 1)];
     const bool some = of_a ? o < (int64_t)slot.rank * a.k : j < slot.rank;
     float v[8], sum = 0.0f;
 #pragma unroll

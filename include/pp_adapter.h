@@ -81,7 +81,7 @@ pp_status_t pp_adapter_project(const pp_adapter_bank_t *bank, const void *x_dev,
 /* Enqueue y = act(Wd x + bias + c B (A x)): x_dev [k][n], y_dev [m][n]; u_dev is scratch that a later
  * pp_adapter_grad_weights can be given.  plan is the layer's pp_block_gemm plan (m, k, dtype equal to the bank's; bias and act
  * are the plan's).  The adapters' part is added before act and before y is rounded.  PP_ERR_SHAPE: n < 1 or above 4194304, k * n or m * n beyond
- * 2^31 - 1, or a plan of another size.  PP_ERR_UNSUPPORTED: another dtype, a host-only bank or plan, a PP_F16 plan with a forced
+ * 2^31 - 1, or a plan of another size or of the transposed weights.  PP_ERR_UNSUPPORTED: another dtype, a host-only bank or plan, a PP_F16 plan with a forced
  * variant (variant 1 has no adapters; variant 2 takes n that are multiples of 8 only).  PP_ERR_ALIGN: misaligned, or an output that overlaps another buffer. */
 pp_status_t pp_adapter_run(const pp_adapter_bank_t *bank, const pp_block_gemm_plan_t *plan, const void *x_dev, const int32_t *slot_of_dev, void *u_dev,
                            void *y_dev, int32_t n, void *hip_stream);
@@ -90,7 +90,8 @@ pp_status_t pp_adapter_run(const pp_adapter_bank_t *bank, const pp_block_gemm_pl
  *   gate_dev   the layer's output y in 8 bits (pp_act8_pack of [m][n]) if the layer has a ReLU: g = dy where y > 0, written to
  *              g_dev [m][n] (dy_dev itself is allowed).  NULL: g = dy, and g_dev is not used.
  *   v_dev      receives v = B^T g
- *   dx_dev     [k][n], from plan_t, a plan of the transposed weights (pp_block_gemm_plan_transposed).  NULL (plan_t is not
+ *   dx_dev     [k][n], from plan_t, the plan of the layer's transposed weights that pp_block_gemm_plan_transposed makes (one of
+ *              pp_block_gemm_plan: PP_ERR_SHAPE, so that a square layer's own plan is not taken for it).  NULL (plan_t is not
  *              used then): no gradient with respect to x is wanted.
  * Refusals as pp_adapter_run. */
 pp_status_t pp_adapter_grad_input(const pp_adapter_bank_t *bank, const pp_block_gemm_plan_t *plan_t, const void *dy_dev, const void *gate_dev, void *g_dev,

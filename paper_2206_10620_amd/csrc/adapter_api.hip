@@ -46,7 +46,7 @@ pp_status_t ready(const pp_adapter_bank_t* b) {
 pp_status_t plan_fits(const pp_adapter_bank_t* b, const pp_block_gemm_plan_t* plan, bool transposed, int32_t n) {
     const BlockPlanFacts f = block_plan_facts(plan);
     if (f.dtype != b->dtype) return PP_ERR_UNSUPPORTED;
-    if (f.m != (transposed ? b->k : b->m) || f.k != (transposed ? b->m : b->k)) return PP_ERR_SHAPE;
+    if (f.m != (transposed ? b->k : b->m) || f.k != (transposed ? b->m : b->k) || f.transposed != transposed) return PP_ERR_SHAPE;
     const pp_status_t st = block_check_adapted(plan, n);
     if (st != PP_OK) return st;
     return !b->on_device || f.device == b->device ? PP_OK : PP_ERR_DEVICE;

@@ -176,7 +176,7 @@ static pp_status_t launch_lists(const pp_block_gemm_plan_t* plan, const void* x_
 namespace ppc {
 
 BlockPlanFacts block_plan_facts(const pp_block_gemm_plan_t* plan) {
-    return {plan->hp.m, plan->hp.k, plan->hp.dtype, (plan->hp.flags & PP_FLAG_RELU) ? 1 : 0, plan->device};
+    return {plan->hp.m, plan->hp.k, plan->hp.dtype, (plan->hp.flags & PP_FLAG_RELU) ? 1 : 0, plan->device, plan->hp.transposed};
 }
 
 pp_status_t block_check_adapted(const pp_block_gemm_plan_t* plan, int32_t n) {

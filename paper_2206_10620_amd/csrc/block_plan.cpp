@@ -154,6 +154,7 @@ pp_status_t build_block_plan_transposed(const pp_block_gemm_desc_t& d, BlockHost
     t.col_keep = cols.empty() ? nullptr : cols.data();
     t.weights = w.data(), t.bias = nullptr;
     t.flags = d.flags & ~(uint32_t)PP_FLAG_RELU;
+    p.transposed = true;
     return build_block_plan(t, p);
 }
 

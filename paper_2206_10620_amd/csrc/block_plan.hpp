@@ -20,6 +20,7 @@ struct BlockHostPlan {
     int dtype = PP_F32;
     int variant = 1;                  // 1 or 2, for every n
     bool forced = false;              // the description named the variant
+    bool transposed = false;          // made by build_block_plan_transposed
     int row_tiles = 0;
     int64_t kept_weights = 0, executed_weights = 0;
     std::vector<int32_t> tile_off;    // [row_tiles + 1] offsets into tile_cols (multiples of kBlockChunk)
@@ -58,6 +59,7 @@ struct K4Expand;
 // and its launch, with the adapters' part added before act (binary16), or without act, which whoever adds them applies (binary32).
 struct BlockPlanFacts {
     int m, k, dtype, relu, device;
+    bool transposed;
 };
 BlockPlanFacts block_plan_facts(const pp_block_gemm_plan_t* plan);
 pp_status_t block_check_adapted(const pp_block_gemm_plan_t* plan, int32_t n);

@@ -11,7 +11,7 @@
  * so a value is off by at most half of 2^e, by less than 2^e where it is below that, and its sign is never
  * lost: q > 0 says of a ReLU's output where the ReLU let through.  Dividing by a power of two is exact: the
  * held values are a function of x alone.  A block with an infinity or a NaN stands for NaN throughout (q keeps the signs,
- * +1 for a NaN).
+ * +1 for a NaN).  Columns that stand for nothing, as a padded batch has them, count like any others: they are set to zero first.
  *
  * The buffer: q as int8 [rows][P], P = n rounded up to a multiple of 128, zeros behind n; then one byte e + 127
  * for each row and block (255: the block stands for NaN) as [P / 128][rows rounded up to a multiple of 16].

@@ -17,9 +17,15 @@
  * contents).  A value outside 0 .. slots - 1 (-1 by convention) and a slot that nothing is loaded into are "no adapter".  Tokens may
  * name slots in any order; tokens of one slot next to each other are fastest.  What an infinity or a NaN in one token's column or in one
  * slot's matrices does stays with that token, with that slot's tokens and with that slot's gradients.
+ * Two things bound that.  Where x was held in 8 bits, 128 neighbouring tokens share a step, whatever their slots: one value that is not finite
+ * makes its row's whole block NaN, and with it that column of dA for every slot with a token in the block; a large one makes the others'
+ * steps coarse.  Columns of padding tokens are set to zero before pp_act8_pack, then they do neither.  And in a PP_F16 bank
+ * products that the formulas make infinite may come out as NaN (an infinity meets both parts of u or v, one of which may be 0), which a
+ * ReLU stores as 0.
  *
  * Storage is the bank's dtype for x, y, dy, g, dx, A and B; sums, u, v and the gradients of A and B are binary32.  In a
- * PP_F16 bank u and v enter products as two binary16 parts with a power of two taken out, which leaves them 20 bits or more.
+ * PP_F16 bank u and v enter products as two binary16 parts with a power of two taken out, which leaves them 20 bits or more,
+ * and 2^-38 of the largest of what shares the power: 16 ranks of a token for y and dx, 128 tokens of a rank for dA and dB.
  *
  * Pointers named *_dev are device pointers to the device the bank was made on, which has to be current, and the plan's
  * (PP_ERR_DEVICE otherwise).  Matrices are row-major without gaps and 16-byte aligned, lists of

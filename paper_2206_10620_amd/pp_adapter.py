@@ -322,7 +322,8 @@ class AdapterBank:
 
     def grad_weights(self, x: Union["Act8", object], u, g, v, slot_of, which, stream: Optional[int] = None):
         """Gradients of the slots that which (int32 tensor) lists: da [count, max_rank, k], db [count, m, max_rank], fp32.  x: the
-        layer's input, as it was or in 8 bits; u of run or project, g and v of grad_input."""
+        layer's input, as it was or in 8 bits (where padding tokens have to be zeros: 128 tokens share a step); u of run or project, g and
+        v of grad_input."""
         torch = _TORCH or _torch()
         _matrix(g, self.m, None, self.dtype, self.device)
         n = g.shape[1]

@@ -78,7 +78,8 @@ pp_status_t pp_adapter_load_many(pp_adapter_bank_t *bank, int32_t count, const i
  * A buffer belongs to the n it was made for.  0 if n is out of range. */
 int64_t pp_adapter_u_bytes(const pp_adapter_bank_t *bank, int32_t n);
 int64_t pp_adapter_v_bytes(const pp_adapter_bank_t *bank, int32_t n);
-/* Scratch memory of pp_adapter_grad_weights for n tokens and count slots (at least 16). */
+/* Scratch memory of pp_adapter_grad_weights for n tokens and count slots (at least 16): about 8 n max_rank bytes a slot up to 256 MB, over
+ * which longer lists are gone through in parts. */
 int64_t pp_adapter_work_bytes(const pp_adapter_bank_t *bank, int32_t n, int32_t count);
 
 /* Enqueue u = A x alone: x_dev [k][n].  What pp_adapter_run leaves in u_dev. */

@@ -344,34 +344,40 @@ pp_status_t pp_adapter_grad_weights(const pp_adapter_bank_t* bank, const void* x
     t.w[0] = sums_of(v_dev, n), t.w[1] = sums_of(u_dev, n);
     t.splits[0] = project_shape(bank->m, n, half, true).splits, t.splits[1] = project_shape(bank->k, n, half, false).splits;
     t.tokens[0] = static_cast<const KxToken*>(v_dev), t.tokens[1] = static_cast<const KxToken*>(u_dev);
-    t.slot_of = slot_of_dev, t.which = which_dev;
+    t.slot_of = slot_of_dev;
     t.n = n, t.blocks = (n + kAct8Block - 1) / kAct8Block, t.rank_pad = bank->rank_pad, t.x_is_act8 = x_is_act8 ? 1 : 0;
-    const dim3 turns((unsigned)t.blocks, (unsigned)count, (unsigned)(2 * (bank->rank_pad / 16)));
-    if (half) hipLaunchKernelGGL(k8_turn<_Float16>, turns, dim3(256), 0, stream, t);
-    else hipLaunchKernelGGL(k8_turn<float>, turns, dim3(256), 0, stream, t);
     K8Grad a{};
     a.in = turned;
     a.x = x_dev, a.g = g_dev;
     a.x_pitch = act8_pitch(n), a.x_scale_pitch = act8_scale_pitch(bank->k);
     a.x_scale = x_is_act8 ? static_cast<const uint8_t*>(x_dev) + bank->k * a.x_pitch : nullptr;
-    a.da = da_dev, a.db = db_dev, a.work = reinterpret_cast<float*>(work + at.sums);
+    a.work = reinterpret_cast<float*>(work + at.sums);
     a.m = bank->m, a.k = bank->k, a.n = n, a.blocks = t.blocks, a.rank_pad = bank->rank_pad, a.max_rank = bank->max_rank;
-    a.tiles_k = sh.tiles_k, a.count = count, a.splits = sh.splits;
-    const dim3 grid((unsigned)(sh.tiles_k + sh.tiles_m), (unsigned)count, (unsigned)sh.splits);
-    if (half) {
-        if (x_is_act8) launch_grad<_Float16, true>(sh.rw, a, grid, stream);
-        else launch_grad<_Float16, false>(sh.rw, a, grid, stream);
-    } else {
-        if (x_is_act8) launch_grad<float, true>(sh.rw, a, grid, stream);
-        else launch_grad<float, false>(sh.rw, a, grid, stream);
-    }
-    if (sh.splits > 1) {
-        K8Join j{};
-        j.slots = turned.slots, j.work = a.work, j.da = da_dev, j.db = db_dev;
-        j.m = bank->m, j.k = bank->k, j.rank_pad = bank->rank_pad, j.max_rank = bank->max_rank, j.count = count, j.splits = sh.splits;
-        j.wgs_a = ((int64_t)bank->k * bank->max_rank + 255) / 256;
-        const int64_t wgs = j.wgs_a + ((int64_t)bank->m * bank->max_rank + 255) / 256;
-        hipLaunchKernelGGL(k8_grad_join, dim3((unsigned)wgs, (unsigned)count), dim3(256), 0, stream, j);
+    a.tiles_k = sh.tiles_k, a.count = at.batch, a.splits = sh.splits;
+    K8Join j{};
+    j.slots = turned.slots, j.work = a.work;
+    j.m = bank->m, j.k = bank->k, j.rank_pad = bank->rank_pad, j.max_rank = bank->max_rank, j.count = at.batch, j.splits = sh.splits;
+    j.wgs_a = ((int64_t)bank->k * bank->max_rank + 255) / 256;
+    for (int from = 0; from < count; from += at.batch) {
+        const unsigned slots = (unsigned)(count - from < at.batch ? count - from : at.batch);
+        t.which = which_dev + from;
+        a.da = j.da = da_dev + (int64_t)from * bank->max_rank * bank->k;
+        a.db = j.db = db_dev + (int64_t)from * bank->max_rank * bank->m;
+        const dim3 turns((unsigned)t.blocks, slots, (unsigned)(2 * (bank->rank_pad / 16)));
+        if (half) hipLaunchKernelGGL(k8_turn<_Float16>, turns, dim3(256), 0, stream, t);
+        else hipLaunchKernelGGL(k8_turn<float>, turns, dim3(256), 0, stream, t);
+        const dim3 grid((unsigned)(sh.tiles_k + sh.tiles_m), slots, (unsigned)sh.splits);
+        if (half) {
+            if (x_is_act8) launch_grad<_Float16, true>(sh.rw, a, grid, stream);
+            else launch_grad<_Float16, false>(sh.rw, a, grid, stream);
+        } else {
+            if (x_is_act8) launch_grad<float, true>(sh.rw, a, grid, stream);
+            else launch_grad<float, false>(sh.rw, a, grid, stream);
+        }
+        if (sh.splits > 1) {
+            const int64_t wgs = j.wgs_a + ((int64_t)bank->m * bank->max_rank + 255) / 256;
+            hipLaunchKernelGGL(k8_grad_join, dim3((unsigned)wgs, slots), dim3(256), 0, stream, j);
+        }
     }
     return launched();
 }

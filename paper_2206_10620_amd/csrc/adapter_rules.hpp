@@ -110,19 +110,27 @@ inline GradShape grad_shape(int m, int k, int n, int count, int rank_pad, bool h
     s.splits = w < 1 ? 1 : (int)w;
     return s;
 }
-// Scratch memory of the gradients: offsets in bytes, multiples of 16.
+// Scratch memory of the gradients: offsets in bytes, multiples of 16.  Every listed slot has room for all tokens in it, so long lists
+// are gone through `batch` slots at a time: as many as 256 MB hold, what the last-level cache does, and one at least.
+constexpr int64_t kGradWork = (int64_t)1 << 28;
 struct GradWork {
+    int batch;
     int64_t masks, w, down, sums, bytes;
 };
 inline GradWork grad_work(int m, int k, int n, int count, int rank_pad, bool half) {
     const int64_t blocks = (n + kAct8Block - 1) / kAct8Block;
     const GradShape s = grad_shape(m, k, n, count, rank_pad, half);
+    // of a slot: K8Slot and K8Mask for v and for u, their operands (two binary16 parts or one binary32), powers of two, shares of the sums
+    const int64_t slots = 2 * 16, masks = 2 * blocks * 32, w = 2 * blocks * rank_pad * kAct8Block * 4, down = half ? 2 * blocks * rank_pad * 4 : 0,
+                  sums = s.splits > 1 ? s.splits * ((int64_t)m + k) * rank_pad * 4 : 0;
+    const int64_t fit = kGradWork / (slots + masks + w + down + sums);
     GradWork o;
-    o.masks = (int64_t)count * 2 * 16;                                   // K8Slot, then K8Mask
-    o.w = o.masks + count * 2 * blocks * 32;
-    o.down = o.w + count * 2 * blocks * rank_pad * kAct8Block * 4;       // two binary16 parts or one binary32
-    o.sums = o.down + (half ? count * 2 * blocks * rank_pad * 4 : 0);
-    o.bytes = o.sums + (s.splits > 1 ? (int64_t)s.splits * count * ((int64_t)m + k) * rank_pad * 4 : 0);
+    o.batch = fit < 1 ? 1 : (fit < count ? (int)fit : count);
+    o.masks = o.batch * slots;
+    o.w = o.masks + o.batch * masks;
+    o.down = o.w + o.batch * w;
+    o.sums = o.down + o.batch * down;
+    o.bytes = o.sums + o.batch * sums;
     return o;
 }
 

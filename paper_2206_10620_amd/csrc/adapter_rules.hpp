@@ -63,6 +63,7 @@ PP_HOST_DEVICE inline int64_t adapter_expand_elems(int width, int rank_pad, bool
 //   slots of rank 16 15.6 / 18.1 / 24.9.  v's projection may also read the gate and write g; a backward pass's whole first half: 1024
 //   tokens of rank 16 49.9 / 46.2 / 48.2, 4096 85.2 / 85.2 / 92.3, of rank 64 101.6 / 116.5 / 136.2.
 constexpr int kProjectWaves = 8;
+constexpr int kAdapterMaxShares = 4;
 struct ProjectShape {
     int ft, tiles, splits;
 };
@@ -72,7 +73,7 @@ inline ProjectShape project_shape(int rows, int n, bool half, bool of_v) {
     s.ft = n <= unit ? 1 : (n <= 4 * unit ? 2 : 4);
     s.tiles = (n + 16 * s.ft - 1) / (16 * s.ft);
     s.splits = 512 / s.tiles;
-    const int steps = (rows + 31) / 32, most = (steps + 2 * kProjectWaves - 1) / (2 * kProjectWaves), limit = n <= (of_v ? 1024 : 512) ? 4 : 2;
+    const int steps = (rows + 31) / 32, most = (steps + 2 * kProjectWaves - 1) / (2 * kProjectWaves), limit = n <= (of_v ? 1024 : 512) ? kAdapterMaxShares : 2;
     if (s.splits > most) s.splits = most;
     if (s.splits > limit) s.splits = limit;
     if (s.splits < 1) s.splits = 1;
@@ -85,9 +86,23 @@ inline int project_subsets(const ProjectShape& s, int slots) {
     if (z > most) z = most;
     return z < 1 ? 1 : z;
 }
+// The first token that tile `tile` loads: the last tile is moved back to end with the last token, unless a lane has one token only (its last
+// lanes repeat the last one then).
+PP_HOST_DEVICE inline int project_first_token(int tile, int n, int ft) {
+    const int own = tile * 16 * ft;
+    return ft == 1 || own < n - 16 * ft ? own : n - 16 * ft;
+}
+
+// u of 32 tokens and 16 ranks stands as the matrix instruction's lanes take it, in two planes of 16 bytes a lane: every load and store of
+// it is a run of 512 bytes or more.  Laid out [token][rank] a lane's load met a line of its own: 4096 x 4096 on 4096 tokens of
+// ranks up to 32 took 2 us more.  The plain offset of (token, rank), of a multiple of four ranks:
+PP_HOST_DEVICE inline int64_t kx_at(int64_t token, int rank, int rank_pad) {
+    return ((token >> 5) * (rank_pad >> 4) + (rank >> 4)) * 512 + ((rank >> 2) & 1) * 256 + (((rank >> 3) & 1) * 32 + (int)(token & 31)) * 4;
+}
+PP_HOST_DEVICE inline int64_t kx_share(int64_t n, int rank_pad) { return (n + 31) / 32 * 32 * rank_pad; }      // elements of a share
 // What a projection leaves: 16 bytes for each token, then the sums, of whole groups of 32 tokens.
 inline int64_t adapter_state_bytes(int rows, int n, int rank_pad, bool half, bool of_v) {
-    return (int64_t)n * 16 + (int64_t)project_shape(rows, n, half, of_v).splits * (((int64_t)n + 31) / 32 * 32) * rank_pad * 4;
+    return (int64_t)n * 16 + project_shape(rows, n, half, of_v).splits * kx_share(n, rank_pad) * 4;
 }
 
 // The gradients of A (k rows of x) and B (m rows of g): a workgroup takes 64 rw rows of one of them and one of `splits` shares of the
@@ -110,6 +125,15 @@ inline GradShape grad_shape(int m, int k, int n, int count, int rank_pad, bool h
     s.splits = w < 1 ? 1 : (int)w;
     return s;
 }
+// A lane loads eight values of a row of z, from `from` on, without a look at the row's end: what follows is another row's, and masked.  Only
+// the matrix's end holds loads back (size: its values, eight or more).  Where that moves a load of which some tokens are there, the block
+// is read again, with a look: always the last block of the tile's last rows.
+PP_HOST_DEVICE inline int64_t grad_load_from(int64_t from, int64_t size) { return from < size - 8 ? from : size - 8; }
+PP_HOST_DEVICE inline bool grad_reads_again(int row0, int tile_rows, int rows, int n) {
+    const int last = row0 + tile_rows - 1 < rows - 1 ? row0 + tile_rows - 1 : rows - 1;
+    return (int64_t)last * n + (n + 7) / 8 * 8 > (int64_t)rows * n;
+}
+
 // Scratch memory of the gradients: offsets in bytes, multiples of 16.  Every listed slot has room for all tokens in it, so long lists
 // are gone through `batch` slots at a time: as many as 256 MB hold, what the last-level cache does, and one at least.
 constexpr int64_t kGradWork = (int64_t)1 << 28;

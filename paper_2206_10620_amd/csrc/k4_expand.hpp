@@ -16,6 +16,8 @@
 
 #include <cstdint>
 
+#include "adapter_rules.hpp"
+
 namespace ppc {
 
 // What a token has: the projection leaves it for whoever reads u, which saves them a load that waits for another.
@@ -25,14 +27,6 @@ struct KxToken {
     float factor;
     int32_t unused;
 };
-
-// u of 32 tokens and 16 ranks stands as the matrix instruction's lanes take it, in two planes of 16 bytes a lane: every load and store of
-// it is a run of 512 bytes or more.  Laid out [token][rank] a lane's load met a line of its own: 4096 x 4096 on 4096 tokens of
-// ranks up to 32 took 2 us more.  The plain offset of (token, rank), of a multiple of four ranks:
-__host__ __device__ __forceinline__ int64_t kx_at(int64_t token, int rank, int rank_pad) {
-    return ((token >> 5) * (rank_pad >> 4) + (rank >> 4)) * 512 + ((rank >> 2) & 1) * 256 + (((rank >> 3) & 1) * 32 + (int)(token & 31)) * 4;
-}
-__host__ __device__ __forceinline__ int64_t kx_share(int64_t n, int rank_pad) { return (n + 31) / 32 * 32 * rank_pad; }      // elements of a share
 
 struct K4Expand {
     const KxToken* tokens;      // [n]

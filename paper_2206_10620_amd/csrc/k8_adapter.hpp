@@ -141,7 +141,7 @@ __global__ __launch_bounds__(64 * kProjectWaves) void k8_project(const K8Project
     const int c = lane & 15, g = lane >> 4;
     const int tile = (int)blockIdx.x / a.splits, split = (int)blockIdx.x - tile * a.splits;
     // The last tile is moved back to end with the last token, or, of one token to a lane, its last lanes repeat that: every load is whole
-    const int own0 = tile * 16 * FT, t0 = FT == 1 ? own0 : min(own0, a.n - 16 * FT);
+    const int own0 = tile * 16 * FT, t0 = project_first_token(tile, a.n, FT);
     const int mine0 = FT == 1 ? min(own0 + c, a.n - 1) : t0 + c * FT;
     const int s0 = (int)((int64_t)a.steps * split / a.splits), s1 = (int)((int64_t)a.steps * (split + 1) / a.splits);
     const int w0 = s0 + (int)((int64_t)(s1 - s0) * wave / W), w1 = s0 + (int)((int64_t)(s1 - s0) * (wave + 1) / W);
@@ -530,8 +530,8 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
     const T* const z_all = static_cast<const T*>(of_a ? a.x : a.g);
     const int64_t z_size = (int64_t)rows * a.n;
     const T* const z_from = z_size < 8 ? static_cast<const T*>(a.in.w) : z_all;             // (too few to read eight: any memory)
-    const int64_t z_most = z_size < 8 ? 0 : z_size - 8;
-    const bool z_again = !(HELD8 && of_a) && (int64_t)min(row0 + 16 * RW - 1, rows - 1) * a.n + (a.n + 7) / 8 * 8 > z_size;
+    const int64_t z_room = z_size < 8 ? 8 : z_size;
+    const bool z_again = !(HELD8 && of_a) && grad_reads_again(row0, 16 * RW, rows, a.n);
     const K8Mask* masks = a.in.masks + ((int64_t)at * 2 + (of_a ? 0 : 1)) * a.blocks;
 
     // 64 blocks at a time, one to a lane; rank and factor are in every block found: the first one's
@@ -600,7 +600,7 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
                 } else {
                     const int64_t from = (int64_t)row * a.n + tb + g * 8;
 #pragma unroll
-                    for (int st = 0; st < 4; ++st) z[i][st] = *reinterpret_cast<const k8_any<T, 8>*>(z_from + min(from + st * 32, z_most));
+                    for (int st = 0; st < 4; ++st) z[i][st] = *reinterpret_cast<const k8_any<T, 8>*>(z_from + grad_load_from(from + st * 32, z_room));
                 }
             }
         };

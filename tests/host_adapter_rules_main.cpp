@@ -1,6 +1,7 @@
 // The adapters' and the 8-bit activations' sizes and launch shapes on the CPU: what keeps their kernels inside their buffers.
 #include <cstdint>
 #include <cstdio>
+#include <vector>
 
 #include "adapter_rules.hpp"
 
@@ -62,8 +63,76 @@ static int grad_works() {
     return 0;
 }
 
+// Projections: every token is some tile's and loaded by it, no tile loads one that is not there, the shares of the rows are nobody's twice,
+// and u holds a place of its own for every token and rank.
+static int projections() {
+    for (int half = 0; half < 2; ++half)
+        for (int of_v = 0; of_v < 2; ++of_v)
+            for (int rows : {1, 31, 32, 33, 511, 512, 513, 1024, 4096, 1 << 22})
+                for (int n = 1; n < 1 << 22; n = n < 4500 ? n + 1 : n * 9 / 8 + 1) {
+                    if ((int64_t)rows * n >= ((int64_t)1 << 31)) break;
+                    const ProjectShape s = project_shape(rows, n, half != 0, of_v != 0);
+                    if (s.ft != 1 && s.ft != 2 && s.ft != 4) return fail("projection: tokens to a lane", rows, n, s.ft);
+                    if (s.splits < 1 || s.splits > kAdapterMaxShares) return fail("projection: shares", rows, n, s.splits);
+                    if ((int64_t)s.tiles * 16 * s.ft < n || ((int64_t)s.tiles - 1) * 16 * s.ft >= n) return fail("projection: tiles", rows, n, s.tiles);
+                    if (s.ft > 1 && n < 16 * s.ft) return fail("projection: a tile of more tokens than there are", rows, n, s.ft);
+                    for (int tile : {0, 1, s.tiles / 2, s.tiles - 2, s.tiles - 1}) {
+                        if (tile < 0 || tile >= s.tiles) continue;
+                        const int first = project_first_token(tile, n, s.ft), own = tile * 16 * s.ft;
+                        if (first < 0 || first > own || (s.ft > 1 && first + 16 * s.ft > n)) return fail("projection: a tile loads past the tokens", rows, n, tile);
+                        if (s.ft > 1 && first != own && tile != s.tiles - 1) return fail("projection: a tile moved that is not the last", rows, n, tile);
+                        const int end = own + 16 * s.ft < n ? own + 16 * s.ft : n;
+                        if (s.ft > 1 && first + 16 * s.ft < end) return fail("projection: a tile's own tokens are not loaded", rows, n, tile);
+                    }
+                    for (int slots : {1, 3, 64, 65536}) {
+                        const int z = project_subsets(s, slots);
+                        if (z < 1 || z > 16 * s.ft || z > slots) return fail("projection: slots dealt out", n, slots, z);
+                    }
+                    for (int rank_pad : {16, 48, 128}) {
+                        const int64_t share = kx_share(n, rank_pad);
+                        if (adapter_state_bytes(rows, n, rank_pad, half != 0, of_v != 0) != (int64_t)n * 16 + s.splits * share * 4) return fail("projection: bytes", rows, n, rank_pad);
+                        // whole groups of eight tokens are read
+                        if (kx_at(((int64_t)n - 1) | 7, rank_pad - 4, rank_pad) + 4 > share) return fail("projection: u ends early", rows, n, rank_pad);
+                    }
+                }
+    std::vector<char> taken;
+    for (int n : {1, 31, 32, 33, 100})
+        for (int rank_pad = 16; rank_pad <= 128; rank_pad += 16) {
+            taken.assign((size_t)kx_share(n, rank_pad), 0);
+            for (int t = 0; t < n; ++t)
+                for (int r = 0; r < rank_pad; r += 4)
+                    for (int e = 0; e < 4; ++e)
+                        if (taken[(size_t)kx_at(t, r, rank_pad) + e]++) return fail("projection: a place twice", t, r, rank_pad);
+        }
+    return 0;
+}
+
+// Gradients: every load of eight values ends inside the matrix, and where one is held back that has tokens, the block is read again.
+static int grad_loads() {
+    for (int rw = 1; rw <= 2; ++rw)
+        for (int rows = 1; rows <= 70; ++rows)
+            for (int n = 1; n <= 300; ++n) {
+                const int64_t size = (int64_t)rows * n, room = size < 8 ? 8 : size;
+                const int blocks = (n + 127) / 128;
+                for (int row0 = 0; row0 < rows; row0 += 16 * rw) {
+                    const bool again = grad_reads_again(row0, 16 * rw, rows, n);
+                    for (int i = 0; i < 16 * rw; ++i) {
+                        const int row = row0 + i < rows ? row0 + i : rows - 1;
+                        for (int t = 0; t < blocks * 128; t += 8) {
+                            const int64_t from = (int64_t)row * n + t, at = grad_load_from(from, room);
+                            if (at < 0 || at + 8 > room) return fail("gradients: a load past the matrix", rows, n, t);
+                            if (at != from && t < n && !again) return fail("gradients: tokens that are not loaded", rows, n, t);
+                            if (at != from && t < n && t / 128 != blocks - 1) return fail("gradients: a block before the last", rows, n, t);
+                            if (size < 8 && t < n && !again) return fail("gradients: a matrix too small to load is not read again", rows, n, t);
+                        }
+                    }
+                }
+            }
+    return 0;
+}
+
 int main() {
-    if (act8_sizes() || grad_works()) return 1;
+    if (act8_sizes() || grad_works() || projections() || grad_loads()) return 1;
     std::printf("ok\n");
     return 0;
 }

@@ -143,7 +143,7 @@ __device__ __forceinline__ uint32_t kx_leaders(int slot) {
 // a branch between the loads that would make each wait for the last, then tile by tile of 32 columns the slots are gone through.
 // Of `parts` wavefronts with the same columns this one takes every by_chunk-th 16 ranks and every by_slot-th slot from my_slot on.
 template <int NT, int D> struct KxItems {
-    static constexpr int kShares = NT == 1 ? 4 : 2;             // of u at once; there are seldom more
+    static constexpr int kShares = NT == 1 ? kAdapterMaxShares : 2;      // of u at once; there are seldom more
     static constexpr int kAtOnce = NT == 4 ? 2 : NT;            // tiles; four would not fit the registers beside their accumulators
     struct Operand {
         kx_h8 v[2];
@@ -172,11 +172,13 @@ template <int NT, int D> struct KxItems {
 #pragma unroll
             for (int b = 1; b < kShares; ++b) v[0][q] += b < e.splits ? w[b][q >> 2][q & 3] : 0.0f;
         }
-        for (int s = kShares; s < e.splits; ++s) {
-            const kx_f4* p = reinterpret_cast<const kx_f4*>(at(s, tile, c));
-            const kx_f4 x = p[0], y = p[64];
+        if constexpr (kShares < kAdapterMaxShares) {
+            for (int s = kShares; s < e.splits; ++s) {
+                const kx_f4* p = reinterpret_cast<const kx_f4*>(at(s, tile, c));
+                const kx_f4 x = p[0], y = p[64];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) v[0][q] += x[q], v[0][4 + q] += y[q];
+                for (int q = 0; q < 4; ++q) v[0][q] += x[q], v[0][4 + q] += y[q];
+            }
         }
     }
 

@@ -338,22 +338,16 @@ __device__ __forceinline__ void k8_expand_tile(const K8Expand& a, int token_tile
     const float* ops0 = a.operands + (int64_t)(row0 + c) * a.rank_pad + 4 * g;
     for (int r0 = 0; r0 < a.rank_pad; r0 += 16) {
         // every lane its own tokens' u, whatever their slots; then slot by slot
-        k8_f4 w[4];
-        for (int s0 = 0; s0 < a.splits; s0 += 4) {
-            k8_f4 v[4][4];
+        k8_f4 w[4], v[kAdapterMaxShares][4];
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
-#pragma unroll
-                for (int f = 0; f < 4; ++f) {
-                    v[b][f] = k8_f4(0.0f);
-                    if (s0 + b < a.splits && f < left) v[b][f] = *reinterpret_cast<const k8_f4*>(a.u + (s0 + b) * a.split_elems + kx_at(t0 + f, r0 + 4 * g, a.rank_pad));
-                }
+        for (int b = 0; b < kAdapterMaxShares; ++b)
 #pragma unroll
             for (int f = 0; f < 4; ++f) {
-                const k8_f4 x = v[0][f] + v[1][f] + v[2][f] + v[3][f];
-                w[f] = s0 ? w[f] + x : x;
+                v[b][f] = k8_f4(0.0f);
+                if (b < a.splits && f < left) v[b][f] = *reinterpret_cast<const k8_f4*>(a.u + b * a.split_elems + kx_at(t0 + f, r0 + 4 * g, a.rank_pad));
             }
-        }
+#pragma unroll
+        for (int f = 0; f < 4; ++f) w[f] = v[0][f] + v[1][f] + v[2][f] + v[3][f];
         int sl[4];
         bool sel[4];
 #pragma unroll

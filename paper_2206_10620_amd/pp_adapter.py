@@ -1,4 +1,6 @@
-"""ctypes binding with the same names as include/pp_adapter.h and include/pp_act8.h (argument marshalling only)."""
+"""ctypes binding with the same names as include/pp_adapter.h and include/pp_act8.h (argument marshalling only).
+
+The library cannot see a tensor's sizes, type or device: they are checked here, by statements that python -O keeps."""
 from __future__ import annotations
 
 import ctypes as C
@@ -75,7 +77,8 @@ def pp_adapter_load(bank, slot: int, rank: int, scale: float, a_dev: int, b_dev:
 
 def pp_adapter_load_many(bank, slots, ranks, scales, a_dev, b_dev, hip_stream: int = 0) -> int:
     """The five sequences have one entry a slot; 0 stands for a null pointer."""
-    assert len(slots) == len(ranks) == len(scales) == len(a_dev) == len(b_dev)
+    if not (len(slots) == len(ranks) == len(scales) == len(a_dev) == len(b_dev)):
+        raise AssertionError("sequences of different lengths")
     lists = array("i", slots), array("i", ranks), array("f", scales), array("Q", a_dev), array("Q", b_dev)
     return lib().pp_adapter_load_many(bank, len(slots), *[t.buffer_info()[0] for t in lists], hip_stream)
 
@@ -169,14 +172,18 @@ def _check_status(st: int, what: str) -> None:
 
 
 def _matrix(t, rows: int, n: Optional[int], dtype: int, device=None):
-    assert t.is_cuda and t.is_contiguous() and t.dim() == 2 and t.dtype == _torch_dtype(dtype) and t.shape[0] == rows
-    assert n is None or t.shape[1] == n
-    assert device is None or t.device == device
+    if not (t.is_cuda and t.is_contiguous() and t.dim() == 2 and t.dtype == _torch_dtype(dtype) and t.shape[0] == rows):
+        raise AssertionError("not a contiguous [rows, n] tensor of the bank's dtype on the GPU")
+    if not (n is None or t.shape[1] == n):
+        raise AssertionError("another number of tokens")
+    if not (device is None or t.device == device):
+        raise AssertionError("on another device")
 
 
 def _opaque_ok(t, device):
     """t is memory of the kind that the calls here leave their state in."""
-    assert t.is_cuda and t.device == device and t.element_size() == 1 and t.is_contiguous()
+    if not (t.is_cuda and t.device == device and t.element_size() == 1 and t.is_contiguous()):
+        raise AssertionError("not memory of the bank's device that a call here left")
 
 
 class Act8:
@@ -185,7 +192,8 @@ class Act8:
     __slots__ = ("buffer", "rows", "n", "dtype")
 
     def __init__(self, buffer, rows: int, n: int, dtype: int):
-        assert 0 < _act8_bytes(rows, n) == buffer.numel()
+        if not (0 < _act8_bytes(rows, n) == buffer.numel()):
+            raise AssertionError("a buffer of another size")
         _opaque_ok(buffer, buffer.device)
         self.buffer, self.rows, self.n, self.dtype = buffer, rows, n, dtype
 
@@ -205,7 +213,8 @@ def act8_pack(x, stream: Optional[int] = None) -> Act8:
     """x [rows, n] (fp16 or fp32, on the GPU) in 8 bits."""
     torch = _TORCH or _torch()
     dtype = PP_F16 if x.dtype == torch.float16 else PP_F32
-    assert x.is_cuda and x.is_contiguous() and x.dim() == 2 and x.dtype == _torch_dtype(dtype)
+    if not (x.is_cuda and x.is_contiguous() and x.dim() == 2 and x.dtype == _torch_dtype(dtype)):
+        raise AssertionError("not a contiguous [rows, n] tensor of fp16 or fp32 on the GPU")
     rows, n = x.shape
     device = x.device
 
@@ -241,7 +250,8 @@ class AdapterBank:
 
     def _slots_of(self, slot_of, n: int):
         torch = _torch()
-        assert slot_of.is_cuda and slot_of.is_contiguous() and slot_of.dtype == torch.int32 and tuple(slot_of.shape) == (n,) and slot_of.device == self.device
+        if not (slot_of.is_cuda and slot_of.is_contiguous() and slot_of.dtype == torch.int32 and tuple(slot_of.shape) == (n,) and slot_of.device == self.device):
+            raise AssertionError("slot_of is a contiguous int32 tensor of a slot for every token, on the bank's device")
 
     def _opaque(self, nbytes: int):
         return _TORCH.empty(nbytes, dtype=_TORCH.uint8, device=self.device)
@@ -256,15 +266,18 @@ class AdapterBank:
 
     def load_many(self, slots: Sequence[int], a, b, scales: Sequence[float], stream: Optional[int] = None) -> None:
         """a[i] [rank, k] and b[i] [m, rank] into slots[i], for all i in one call (in their order, where a slot stands twice; no slots: nothing)."""
-        assert len(slots) == len(a) == len(b) == len(scales)
+        if not (len(slots) == len(a) == len(b) == len(scales)):
+            raise AssertionError("sequences of different lengths")
         if not len(slots):
             return
         tdt, index, t = _torch_dtype(self.dtype), self.device.index, _TORCH.Tensor
         both = [*a, *b]                            # a list of 64 slots takes 60 us to look over one tensor after another, 45 check by check
         sizes = list(map(t.size, a))
         ranks = [s[0] if len(s) == 2 else -1 for s in sizes]
-        assert sizes == [(r, self.k) for r in ranks] and list(map(t.size, b)) == [(self.m, r) for r in ranks]
-        assert all([x.dtype is tdt for x in both]) and set(map(t.get_device, both)) == {index} and all(map(t.is_contiguous, both))
+        if not (sizes == [(r, self.k) for r in ranks] and list(map(t.size, b)) == [(self.m, r) for r in ranks]):
+            raise AssertionError("a is [rank, k] and b [m, rank]")
+        if not (all([x.dtype is tdt for x in both]) and set(map(t.get_device, both)) == {index} and all(map(t.is_contiguous, both))):
+            raise AssertionError("a and b are contiguous tensors of the bank's dtype on its device")
         at = list(map(t.data_ptr, both))
         _on(self.device, stream, lambda s: _check_status(
             pp_adapter_load_many(self.handle, slots, ranks, scales, at[:len(a)], at[len(a):], s), "pp_adapter_load_many"))
@@ -306,7 +319,8 @@ class AdapterBank:
         _matrix(dy, self.m, None, self.dtype, self.device)
         n = dy.shape[1]
         self._slots_of(slot_of, n)
-        assert gate is None or (gate.rows == self.m and gate.n == n and gate.buffer.device == self.device)
+        if not (gate is None or (gate.rows == self.m and gate.n == n and gate.buffer.device == self.device)):
+            raise AssertionError("the gate is the output [m, n] in 8 bits, on the bank's device")
 
         def call(s):
             torch = _TORCH
@@ -330,11 +344,14 @@ class AdapterBank:
         self._slots_of(slot_of, n)
         held = isinstance(x, Act8)
         if held:
-            assert x.rows == self.k and x.n == n and x.buffer.device == self.device
+            if not (x.rows == self.k and x.n == n and x.buffer.device == self.device):
+                raise AssertionError("x is the input [k, n], on the bank's device")
         else:
             _matrix(x, self.k, n, self.dtype, self.device)
-        assert which.is_cuda and which.is_contiguous() and which.dtype == torch.int32 and which.dim() == 1 and which.device == self.device
-        assert (u.numel(), v.numel()) == self._state_bytes(n)
+        if not (which.is_cuda and which.is_contiguous() and which.dtype == torch.int32 and which.dim() == 1 and which.device == self.device):
+            raise AssertionError("which is a contiguous int32 tensor on the bank's device")
+        if not ((u.numel(), v.numel()) == self._state_bytes(n)):
+            raise AssertionError("u and v are those of this many tokens")
         _opaque_ok(u, self.device)
         _opaque_ok(v, self.device)
         count = which.shape[0]

@@ -567,12 +567,13 @@ __global__ __launch_bounds__(256) void k8_grad(const K8Grad a) {
         if (todo > 0) {
             int over = skip;
             left = found0;
-            while (__builtin_popcountll(left) <= over) over -= __builtin_popcountll(left), left = found(++group);
+            while (__builtin_popcountll(left) <= over && group + 1 < groups) over -= __builtin_popcountll(left), left = found(++group);
             for (; over > 0; --over) left &= left - 1;
         }
-        auto next_block = [&]() {                                // called `todo` times only
-            while (left == 0) left = found(++group);
-            const int b = group * 64 + __builtin_ctzll(left);
+        // called `todo` times only; it ends, in a block that there is, also where another call writes to the scratch memory meanwhile
+        auto next_block = [&]() {
+            while (left == 0 && group + 1 < groups) left = found(++group);
+            const int b = group * 64 + (left ? __builtin_ctzll(left) : 0);
             left &= left - 1;
             return b;
         };

@@ -331,7 +331,7 @@ pp_status_t pp_adapter_grad_weights(const pp_adapter_bank_t* bank, const void* x
     const pp_status_t st = ready(bank);
     if (st != PP_OK) return st;
     const bool half = bank->dtype == PP_F16;
-    const GradShape sh = grad_shape(bank->m, bank->k, n, count, bank->rank_pad, half);
+    const GradShape sh = grad_shape(bank->m, bank->k, n, count, bank->rank_pad, half, x_is_act8 != 0);
     const GradWork at = grad_work(bank->m, bank->k, n, count, bank->rank_pad, half);
     char* work = static_cast<char*>(work_dev);
     K8Turned turned;

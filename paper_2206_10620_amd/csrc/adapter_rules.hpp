@@ -108,14 +108,24 @@ inline int64_t adapter_state_bytes(int rows, int n, int rank_pad, bool half, boo
 // The gradients of A (k rows of x) and B (m rows of g): a workgroup takes 64 rw rows of one of them and one of `splits` shares of the
 // blocks of 128 tokens.  Shares fill the GPU but cost a launch that joins them, 4 us.  4096 + 4096 rows of one slot, 1 / 2 / 4 / 8 shares:
 // 4096 tokens 38.4 / 26.5 / 22.7 / 24.0 us, 512 10.2 / 11.2 / 11.5 / 14.2.  1024 + 4096 rows, 2000 tokens of six slots of rank 64: 29.8 /
-// 35.0 / 35.4 / 44.6.  Rank 64 is read from the cache once for every 16 rw rows, so long sums take rw 2: 34.9 us against 39.3.
+// 35.0 / 35.4 / 44.6.  Ranks above 32 are read from the cache once for every 16 rw rows, so long sums take rw 2 where its half as many
+// workgroups still fill the GPU: more of them for binary32 and for x from 8 bits, of which two row tiles leave room for one wavefront to a
+// SIMD.  Rank 64, rw 1 / 2, the workgroups that rw 1 has in front (ranks 48 and 128 turn at the same places):
+//                                   binary16 x    binary16, 8 bits   binary32 x    binary32, 8 bits
+//   128: 4096 + 4096 rows,  4096 t  38.6 / 35.8   38.8 / 40.9        65.2 / 69.1   65.2 / 68.4 us
+//        the same,         16384 t  155 / 111     115 / 106          216 / 210     212 / 221
+//    80: 1024 + 4096 rows, 16384 t  84.2 / 81.6   79.7 / 101         153 / 206     143 / 192
+//    32: 1024 + 1024 rows, 16384 t  42.9 / 59.1   43.0 / 60.1        63.2 / 109    63.9 / 111
+//   512: 4096 + 4096, four slots    155 / 118     117 / 116          215 / 220     213 / 230
+//   320: 1024 + 4096, four slots    113 / 71.4    107 / 85.3         208 / 163     197 / 152
 struct GradShape {
     int rw, tiles_k, tiles_m, splits;
 };
-inline GradShape grad_shape(int m, int k, int n, int count, int rank_pad, bool half) {
+inline GradShape grad_shape(int m, int k, int n, int count, int rank_pad, bool half, bool x_is_act8) {
     GradShape s;
     const int64_t blocks = (n + kAct8Block - 1) / kAct8Block, each = (blocks + count - 1) / count;      // a slot's, if they are alike
-    s.rw = rank_pad > 32 && each >= 16 ? 2 : 1;
+    const int64_t small = (int64_t)((k + 63) / 64 + (m + 63) / 64) * count;
+    s.rw = rank_pad > 32 && each >= 16 && small >= (half && !x_is_act8 ? 128 : 256) ? 2 : 1;
     s.tiles_k = (k + 64 * s.rw - 1) / (64 * s.rw);
     s.tiles_m = (m + 64 * s.rw - 1) / (64 * s.rw);
     const int64_t wgs = (int64_t)(s.tiles_k + s.tiles_m) * count;
@@ -134,8 +144,8 @@ PP_HOST_DEVICE inline bool grad_reads_again(int row0, int tile_rows, int rows, i
     return (int64_t)last * n + (n + 7) / 8 * 8 > (int64_t)rows * n;
 }
 
-// Scratch memory of the gradients: offsets in bytes, multiples of 16.  Every listed slot has room for all tokens in it, so long lists
-// are gone through `batch` slots at a time: as many as 256 MB hold, what the last-level cache does, and one at least.
+// Scratch memory of the gradients, x as it is or in 8 bits: offsets in bytes, multiples of 16.  Every listed slot has room for all tokens in
+// it, so long lists are gone through `batch` slots at a time: as many as 256 MB hold, what the last-level cache does, and one at least.
 constexpr int64_t kGradWork = (int64_t)1 << 28;
 struct GradWork {
     int batch;
@@ -143,10 +153,11 @@ struct GradWork {
 };
 inline GradWork grad_work(int m, int k, int n, int count, int rank_pad, bool half) {
     const int64_t blocks = (n + kAct8Block - 1) / kAct8Block;
-    const GradShape s = grad_shape(m, k, n, count, rank_pad, half);
+    const int as_it_is = grad_shape(m, k, n, count, rank_pad, half, false).splits, held = grad_shape(m, k, n, count, rank_pad, half, true).splits;
+    const int splits = as_it_is > held ? as_it_is : held;
     // of a slot: K8Slot and K8Mask for v and for u, their operands (two binary16 parts or one binary32), powers of two, shares of the sums
     const int64_t slots = 2 * 16, masks = 2 * blocks * 32, w = 2 * blocks * rank_pad * kAct8Block * 4, down = half ? 2 * blocks * rank_pad * 4 : 0,
-                  sums = s.splits > 1 ? s.splits * ((int64_t)m + k) * rank_pad * 4 : 0;
+                  sums = splits > 1 ? splits * ((int64_t)m + k) * rank_pad * 4 : 0;
     const int64_t fit = kGradWork / (slots + masks + w + down + sums);
     GradWork o;
     o.batch = fit < 1 ? 1 : (fit < count ? (int)fit : count);

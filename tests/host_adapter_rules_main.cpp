@@ -46,19 +46,21 @@ static int grad_works() {
                     for (int rank_pad = 16; rank_pad <= 128; rank_pad += 16)
                         for (int half = 0; half < 2; ++half) {
                             if ((int64_t)m * k >= ((int64_t)1 << 31) || (int64_t)m * n >= ((int64_t)1 << 31) || (int64_t)k * n >= ((int64_t)1 << 31)) continue;
-                            const GradShape s = grad_shape(m, k, n, count, rank_pad, half != 0);
-                            const GradWork w = grad_work(m, k, n, count, rank_pad, half != 0);
-                            const int64_t blocks = (n + 127) / 128;
-                            if (s.splits < 1 || s.splits > 8 || s.splits > blocks) return fail("gradients: shares", m, n, s.splits);
-                            if (s.rw < 1 || s.rw > 2 || (int64_t)s.tiles_k * 64 * s.rw < k || (int64_t)s.tiles_m * 64 * s.rw < m) return fail("gradients: tiles", m, k, s.rw);
-                            if (w.batch < 1 || w.batch > count) return fail("gradients: slots at a time", m, count, w.batch);
-                            if (w.masks % 16 || w.w % 16 || w.down % 16 || w.sums % 16) return fail("gradients: alignment", m, n, count);
-                            if (w.masks < (int64_t)w.batch * 2 * 16 || w.w - w.masks < w.batch * 2 * blocks * 32) return fail("gradients: masks", m, n, count);
-                            if (w.down - w.w < w.batch * 2 * blocks * rank_pad * 512) return fail("gradients: operands", m, n, count);
-                            if (w.sums - w.down < (half ? w.batch * 2 * blocks * rank_pad * 4 : 0)) return fail("gradients: powers of two", m, n, count);
-                            if (w.bytes - w.sums < (s.splits > 1 ? (int64_t)s.splits * w.batch * ((int64_t)m + k) * rank_pad * 4 : 0)) return fail("gradients: sums", m, n, count);
-                            if (w.batch > 1 && w.bytes > kGradWork) return fail("gradients: more than the bound", m, n, w.batch);
-                            if (w.batch < count && w.bytes / w.batch * (w.batch + 1) + 1024 < kGradWork) return fail("gradients: less than would fit", m, n, w.batch);
+                            for (int held = 0; held < 2; ++held) {
+                                const GradShape s = grad_shape(m, k, n, count, rank_pad, half != 0, held != 0);
+                                const GradWork w = grad_work(m, k, n, count, rank_pad, half != 0);
+                                const int64_t blocks = (n + 127) / 128;
+                                if (s.splits < 1 || s.splits > 8 || s.splits > blocks) return fail("gradients: shares", m, n, s.splits);
+                                if (s.rw < 1 || s.rw > 2 || (int64_t)s.tiles_k * 64 * s.rw < k || (int64_t)s.tiles_m * 64 * s.rw < m) return fail("gradients: tiles", m, k, s.rw);
+                                if (w.batch < 1 || w.batch > count) return fail("gradients: slots at a time", m, count, w.batch);
+                                if (w.masks % 16 || w.w % 16 || w.down % 16 || w.sums % 16) return fail("gradients: alignment", m, n, count);
+                                if (w.masks < (int64_t)w.batch * 2 * 16 || w.w - w.masks < w.batch * 2 * blocks * 32) return fail("gradients: masks", m, n, count);
+                                if (w.down - w.w < w.batch * 2 * blocks * rank_pad * 512) return fail("gradients: operands", m, n, count);
+                                if (w.sums - w.down < (half ? w.batch * 2 * blocks * rank_pad * 4 : 0)) return fail("gradients: powers of two", m, n, count);
+                                if (w.bytes - w.sums < (s.splits > 1 ? (int64_t)s.splits * w.batch * ((int64_t)m + k) * rank_pad * 4 : 0)) return fail("gradients: sums", m, n, count);
+                                if (w.batch > 1 && w.bytes > kGradWork) return fail("gradients: more than the bound", m, n, w.batch);
+                                if (w.batch < count && w.bytes / w.batch * (w.batch + 1) + 1024 < kGradWork) return fail("gradients: less than would fit", m, n, w.batch);
+                            }
                         }
     return 0;
 }

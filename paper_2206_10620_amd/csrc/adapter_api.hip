@@ -137,8 +137,11 @@ pp_status_t launch_product(const pp_adapter_bank_t* b, bool of_b, const pp_block
     a.slot_elems = (of_b ? b->b_expand_slot : b->a_expand_slot) / 4;
     a.split_elems = split_elems;
     a.m = of_b ? b->m : b->k, a.n = n, a.splits = splits, a.rank_pad = b->rank_pad, a.relu = block_plan_facts(plan).relu;
-    const int token_tiles = (n + 63) / 64;
-    hipLaunchKernelGGL(k8_expand_f32, dim3((unsigned)((a.m + 63) / 64), (unsigned)(token_tiles < 32768 ? token_tiles : 32768)), dim3(256), 0, stream, a);
+    const bool few = expand_few(a.m, n, b->slots);
+    const int token_tiles = few ? (n + 15) / 16 : (n + 63) / 64;
+    const dim3 grid((unsigned)(few ? (a.m + 15) / 16 : (a.m + 63) / 64), (unsigned)(token_tiles < 32768 ? token_tiles : 32768));
+    if (few) hipLaunchKernelGGL(k8_expand_few, grid, dim3(64 * kExpandWaves), 0, stream, a);
+    else hipLaunchKernelGGL(k8_expand_f32, grid, dim3(256), 0, stream, a);
     return PP_OK;
 }
 

@@ -105,6 +105,17 @@ inline int64_t adapter_state_bytes(int rows, int n, int rank_pad, bool half, boo
     return (int64_t)n * 16 + project_shape(rows, n, half, of_v).splits * kx_share(n, rank_pad) * 4;
 }
 
+// The expansion in binary32: 64 tokens and 16 rows to a wavefront, which goes through the tokens' slots one by one, or 16 tokens and 16 rows to
+// a workgroup, whose four wavefronts share slots and ranks.  The first reads B once for four times as many tokens, the second is done
+// soon where tokens name many slots, and fills the GPU where there is little to do.  The expansion alone, m x n, rank 8 / 128, first and second:
+//   one slot    1024 x 1 3.4 / 12.0, 3.3 / 3.9 us   1024 x 256 3.6 / 12.7, 3.4 / 9.7   4096 x 128 4.4 / 14.5, 6.7 / 19.1   1024 x 1024 5.4 / 16, 12 / 37
+//   64 slots    1024 x 64 39 / 353, 3.9 / 12.2      4096 x 128 30 / 198, 11 / 29       1024 x 1024 9.6 / 46, 14 / 36       4096 x 1024 24 / 107, 48 / 130
+// and with 64 slots in no order 1024 x 1024 27 / 185, 19 / 64, 4096 x 1024 69 / 541, 63 / 244.
+constexpr int kExpandWaves = 4;
+inline bool expand_few(int m, int n, int slots) {
+    return (int64_t)((m + 15) / 16) * ((n + 15) / 16) <= (slots > 16 ? 4096 : 1024);
+}
+
 // The gradients of A (k rows of x) and B (m rows of g): a workgroup takes 64 rw rows of one of them and one of `splits` shares of the
 // blocks of 128 tokens.  Shares fill the GPU but cost a launch that joins them, 4 us.  4096 + 4096 rows of one slot, 1 / 2 / 4 / 8 shares:
 // 4096 tokens 38.4 / 26.5 / 22.7 / 24.0 us, 512 10.2 / 11.2 / 11.5 / 14.2.  1024 + 4096 rows, 2000 tokens of six slots of rank 64: 29.8 /

@@ -375,6 +375,85 @@ __device__ __forceinline__ void k8_expand_tile(const K8Expand& a, int token_tile
         k8_store<float, 4>(a.y + (int64_t)(row0 + 4 * g + i) * a.n + t0, row0 + 4 * g + i < a.m ? left : 0, y[i]);
     }
 }
+// The same for 16 tokens, one to a lane, which name 16 slots at most: a workgroup takes 16 rows, and its wavefronts deal the ranks out among
+// them, 16 at a time, then the slots; what each adds up is joined through LDS in order.  B of kExpandAhead slots is on its way at a time: slot by
+// slot, each waiting for its B, 64 tokens of 64 slots of rank 128 took 350 us, 12 here.
+constexpr int kExpandAhead = 8;
+__device__ __forceinline__ void k8_expand_few_tile(const K8Expand& a, int token_tile, k8_f4* red) {
+    const int lane = (int)(threadIdx.x & 63u), wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int c = lane & 15, g = lane >> 4;
+    const int row0 = (int)blockIdx.x * 16, t = token_tile * 16 + c;
+    KxToken tok = {-1, 0, 0.0f, 0};
+    if (t < a.n) tok = a.tokens[t];
+    float* y = a.y + (int64_t)(row0 + 4 * g) * a.n + t;
+    float old[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        old[i] = 0.0f;
+        if (wave == 0 && t < a.n && row0 + 4 * g + i < a.m) old[i] = y[(int64_t)i * a.n];
+    }
+    const uint32_t leaders = kx_leaders(tok.slot);
+    if (!a.relu && leaders == 0) return;
+    const int tiles = a.rank_pad / 16, row = min(row0 + c, a.m - 1);
+    int by_chunk = 1;
+    while (by_chunk < kExpandWaves && 2 * by_chunk <= tiles) by_chunk *= 2;
+    const int my_slot = wave / by_chunk, by_slot = kExpandWaves / by_chunk;
+    const float* ops0 = a.operands + (int64_t)row * a.rank_pad + 4 * g;
+    const int tu = min(t, a.n - 1);
+    k8_f4 sum = k8_f4(0.0f);
+    for (int chunk = wave % by_chunk; chunk < tiles; chunk += by_chunk) {
+        uint32_t left = leaders & (uint32_t)__builtin_amdgcn_ballot_w64(tok.rank > chunk * 16);
+        for (int i = 0; i < my_slot; ++i) left &= left - 1;
+        if (left == 0) continue;
+        k8_f4 v[kAdapterMaxShares], op[kExpandAhead];
+#pragma unroll
+        for (int b = 0; b < kAdapterMaxShares; ++b)
+            v[b] = *reinterpret_cast<const k8_f4*>(a.u + (b < a.splits ? b : 0) * a.split_elems + kx_at(tu, chunk * 16 + 4 * g, a.rank_pad));
+        k8_f4 w = v[0];
+        bool first = true;
+        while (left) {
+            int slot[kExpandAhead];
+#pragma unroll
+            for (int d = 0; d < kExpandAhead; ++d) {
+                slot[d] = left ? __builtin_amdgcn_readlane(tok.slot, __builtin_ctz(left)) : -1;
+                for (int i = 0; i < by_slot; ++i) left &= left - 1;
+                op[d] = *reinterpret_cast<const k8_f4*>(ops0 + (slot[d] < 0 ? slot[0] : slot[d]) * a.slot_elems + chunk * 16);
+            }
+            if (first) {
+#pragma unroll
+                for (int b = 1; b < kAdapterMaxShares; ++b)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] += b < a.splits ? v[b][i] : 0.0f;
+                first = false;
+            }
+#pragma unroll
+            for (int d = 0; d < kExpandAhead; ++d) {
+                if (slot[d] < 0) break;
+                k8_f4 acc = k8_f4(0.0f);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(op[d][i], w[i], acc, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] = tok.slot == slot[d] ? __builtin_fmaf(acc[i], tok.factor, sum[i]) : sum[i];
+            }
+        }
+    }
+    __syncthreads();                                             // what was there has been read
+    red[wave * 64 + lane] = sum;
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int w = 1; w < kExpandWaves; ++w) sum += red[w * 64 + lane];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float v = old[i] + sum[i];
+        if (a.relu) v = v > 0.0f ? v : 0.0f;
+        if (t < a.n && row0 + 4 * g + i < a.m) y[(int64_t)i * a.n] = v;
+    }
+}
+__global__ __launch_bounds__(64 * kExpandWaves) void k8_expand_few(const K8Expand a) {
+    __shared__ k8_f4 red[kExpandWaves * 64];
+    for (int tile = (int)blockIdx.y; tile * 16 < a.n; tile += (int)gridDim.y) k8_expand_few_tile(a, tile, red);
+}
 __global__ __launch_bounds__(256) void k8_expand_f32(const K8Expand a) {
     for (int tile = (int)blockIdx.y; tile * 64 < a.n; tile += (int)gridDim.y) k8_expand_tile(a, tile);
 }

@@ -5,7 +5,7 @@
 // which is how u lies in memory: no staging.  They enter as two binary16 parts, hi and lo, after a power of two that brings the
 // token's largest |u| of 16 ranks to [2^14, 2^15) is taken out: 20 bits, whatever the size of u, where y keeps 11.  B lies in operand
 // order, 1 KB per 32 rows and 16 ranks.
-// What it costs is reading u, once for every 64 rows of y: 4096 x 1024 at 0.17 on 2048 tokens takes 17 us without adapters, 5, 7, 13 and
+// What it costs is reading u, once for every 64 rows of y: 4096 x 1024 at 0.17 on 2048 tokens takes 18 us without adapters, 4, 7, 13 and
 // 24 more with rank 16, 32, 64 and 128 (two shares of u, 8 bytes a token and rank, are four times a row of x).
 //
 // The tokens of a wavefront are taken slot by slot.  A matrix instruction computes all its columns with the one slot's B;

@@ -107,6 +107,23 @@ def test_loading_before_the_backward_pass(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_tokens_named_for_another_slot_since_count_for_neither(dtype):
+    """u and v of such a token are the old slot's: it is left out of both sums, and of no other's."""
+    p = Problem(dtype, 64, 50, 300, [8, 24, 5], 24, "mixed", seed=6)
+    s = Step(p)
+    s.project()
+    s.grad_input()
+    old = p.slot_of.copy()
+    p.slot_of[:200:3] = (p.slot_of[:200:3] + 2) % 4 - 1                        # the next one, or none after the last
+    s.slot_of.copy_(dev(p.slot_of))
+    da, db = s.grad_weights()
+    p.slot_of[p.slot_of != old] = -1
+    (_, want_a, want_b), (_, room_a, room_b) = p.backward(p.x, None, range(3))
+    assert_within(da.cpu().numpy(), want_a, room_a, "dA")
+    assert_within(db.cpu().numpy(), want_b, room_b, "dB")
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
 def test_a_slot_far_behind_the_first_tokens(dtype):
     """Blocks are found 64 at a time: a slot whose first token is in the second of those runs, and one that has tokens in each of three."""
     p = Problem(dtype, 33, 40, 20000, [6, 17, 9], 20, "none", seed=4)
